@@ -18,9 +18,13 @@ template <typename ALLOC, size_t BYTES, int KEEP> struct HostBlock {
             for (void*& k : kept())
                 if (k) { p = k; k = nullptr; pinned = true; return; }
         }
+        // Ordinary memory first: where there is none, the runtime (whose first use may be this) is not asked, as it throws then.
+        void* const spare = ::operator new(BYTES, std::nothrow);
+        if (!spare) return;
         p = ALLOC::pin(BYTES);
         pinned = p != nullptr;
-        if (!pinned) p = ::operator new(BYTES, std::nothrow);
+        if (pinned) ::operator delete(spare);
+        else p = spare;
     }
     ~HostBlock()
     {
