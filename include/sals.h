@@ -431,6 +431,94 @@ sals_status sals_calib_eigenvectors(double* C, int32_t D, int32_t r, int32_t dty
                                     void* workspace, size_t workspace_bytes, int32_t max_sweeps, int32_t* sweeps,
                                     void* hip_stream);
 
+/* ---- paged key-value cache of uncompressed layers ---------------------------------------------------
+ * The dense cache of sals_dense_attend in pages, for layers that stay uncompressed and as the ground of the other way to
+ * make decode attention sparse: dropping tokens for good once they have gathered little attention.  Three calls on a
+ * context of their own: append new tokens, attend with one new token per sequence, evict.
+ *
+ * The cache of one layer.  K and V each are a pool of n_pages pages of page_size rows [H_kv, d] T; page p starts at
+ * element p * page_stride of the pool (so that K and V, or several layers, can share one allocation).  Slot j of
+ * sequence b is row j % page_size of page
+ *   table [B, max_pages] int32:  table[b, j / page_size].
+ * seq_len[b] slots are in use (seq_len is clamped to [0, max_pages * page_size]).  An entry outside [0, n_pages) is a
+ * page that is not there: append drops the tokens that belong there (their slots are counted), attend gives them no weight,
+ * evict neither reads nor writes their rows.  Entries of slots at or past the length are not read by attend.
+ * The context holds no cache state: one context serves all layers of a shape.
+ *
+ * Accumulated attention weights (weight_heads: 0 none, 1 one per slot, H_kv one per slot and KV head):
+ *   weights [B, weight_heads, max_pages * page_size] fp32   sum over the steps, and over the query heads that share
+ *                                                           it, of the softmax weight that the slot was given
+ *   pos     [B, weight_heads, max_pages * page_size] int32  RoPE position of the token in the slot
+ * With H_kv lists every head's part [d] of a slot's row may hold another token; K is stored rotated, so the order of
+ * the slots is free. */
+typedef struct {
+    int32_t B;            /* sequences per call, 1 .. 1024                                  */
+    int32_t H_q;          /* query heads, a multiple of H_kv, at most 1024                  */
+    int32_t H_kv;         /* key/value heads                                                */
+    int32_t d;            /* head width: 64 | 128                                           */
+    int32_t page_size;    /* rows of a page, 1 .. 2048                                      */
+    int32_t max_pages;    /* entries of a sequence's table; max_pages * page_size <= 2^20   */
+    int32_t n_pages;      /* pages of the pool                                              */
+    int32_t weight_heads; /* 0 | 1 | H_kv                                                   */
+    int64_t page_stride;  /* elements from page to page: at least page_size * H_kv * d and a multiple of 16 bytes; 0: exactly that */
+    float   rope_theta;   /* as in sals_desc                                                */
+    int32_t rope_style;
+    int32_t dtype;
+} sals_paged_desc;
+
+typedef struct sals_paged sals_paged;   /* opaque host object: descriptor + workspace pointer */
+
+/* Bytes of device workspace.  With weight_heads > 0 most of it are the logits of a step, B * H_q * max_pages * page_size * 4.
+ * Host-only. */
+sals_status sals_paged_workspace_bytes(const sals_paged_desc* desc, size_t* bytes);
+
+/* As sals_create.  Host-only; the context can be used once sals_paged_prepare has returned. */
+sals_status sals_paged_create(const sals_paged_desc* desc, void* d_workspace, size_t workspace_bytes, sals_paged** out);
+void sals_paged_destroy(sals_paged* ctx);
+
+/* One-time device set-up: clears the workspace's arrival counts with a kernel on `hip_stream` and WAITS for it.  Afterwards
+ * the calls below may come from any stream, ordered with each other, and may be captured into HIP graphs; before, they
+ * return SALS_ERR_INVALID_ARG.  Calling it again, with no call in flight, makes the counts right again after a launch that
+ * failed. */
+sals_status sals_paged_prepare(sals_paged* ctx, void* hip_stream);
+
+/* New tokens enter the cache.  For t < n_new[b], slot j = seq_len[b] + t:
+ *   K[j] = RoPE(k_new[b, t], q_pos[b] + t),  V[j] = v_new[b, t],  pos[b, :, j] = q_pos[b] + t,  weights[b, :, j] = 0
+ * then seq_len[b] += n_new[b].  Tokens past slot max_pages * page_size are dropped and the length stops there.
+ *   k_new, v_new [B, n_tok, H_kv, d] T   pre-RoPE keys / values
+ *   q_pos        [B] int32               position of the first new token
+ *   n_new        [B] int32               tokens of each sequence, clamped to [0, n_tok]; NULL: n_tok everywhere
+ *   n_tok        1 .. 2^20 (host)
+ *   pos, weights                         NULL exactly if weight_heads == 0 */
+sals_status sals_paged_append(sals_paged* ctx, const void* k_new, const void* v_new, const int32_t* q_pos, const int32_t* table,
+                              void* Kp, void* Vp, int32_t* seq_len, const int32_t* n_new, int32_t n_tok, int32_t* pos,
+                              float* weights, void* hip_stream);
+
+/* Dense attention of one new token per sequence over its cached slots (sals_dense_attend over pages):
+ *   p[h, j]   = softmax_j( RoPE(q[b,h], q_pos[b]) . K[j, g(h)] / sqrt(d) ),  j < seq_len[b], page there
+ *   out[b, h] = sum_j p[h, j] V[j, g(h)]           fp32 accumulation, one rounding to T; zero where no slot has a page
+ *   weights[b, a, j] += sum over the query heads h of a of p[h, j]    (in head order, fp32)
+ * `weights` may be NULL: then none are added up.  Results do not depend on the order in which workgroups run.
+ *   q [B, H_q, d] T pre-RoPE;  q_pos [B] int32;  out [B, H_q, d] T */
+sals_status sals_paged_attend(sals_paged* ctx, const void* q, const int32_t* q_pos, const int32_t* table, const void* Kp,
+                              const void* Vp, const int32_t* seq_len, float* weights, void* out, void* hip_stream);
+
+/* Eviction by accumulated attention weight: every sequence longer than n_keep keeps n_keep slots (of every list: all
+ * heads' rows with weight_heads == 1, each KV head's with H_kv).  A list's slots are ranked by
+ *   protected before not (pos < n_sink, or pos > q_pos[b] - n_recent), then the larger weight (-0 equals +0, NaN below all),
+ *   then the lower slot,
+ * and the first n_keep stay.  Those among them at slots >= n_keep move into the slots below n_keep that became free, the
+ * i-th of the ones into the i-th of the others in slot order: rows of K and V, pos and weights.  Then
+ * seq_len[b] = n_keep, and the pages from slot n_keep on may be given to other sequences.  Nothing else is written; a
+ * sequence of at most n_keep slots stays as it is.  Pages that more than one sequence reads must not be among those moved into.
+ *   q_pos  [B] int32                          position of the sequence's newest token
+ *   n_keep 1 .. max_pages * page_size;  n_sink, n_recent >= 0 (host)
+ *   src    [B, weight_heads, n_keep] int32    out, may be NULL: the slot that the token now in slot j came from; -1 from
+ *                                             the (new) length on */
+sals_status sals_paged_evict(sals_paged* ctx, const int32_t* q_pos, const int32_t* table, void* Kp, void* Vp, int32_t* seq_len,
+                             int32_t* pos, float* weights, int32_t n_keep, int32_t n_sink, int32_t n_recent, int32_t* src,
+                             void* hip_stream);
+
 /* ---- measurement aid --------------------------------------------------------------
  * Per-stage timing for roofline figures.  While enabled, every stage below (one kernel;
  * for the selection of long sequences a chain of two or three, or of four on its own,

@@ -34,6 +34,8 @@ EXPORTS = (
     "sals_window_append_qv", "sals_sparse_attend_qv_window", "sals_decode_step_qv_window",
     "sals_calib_accumulate_workspace_bytes", "sals_calib_accumulate",
     "sals_calib_eigenvectors_workspace_bytes", "sals_calib_eigenvectors",
+    "sals_paged_workspace_bytes", "sals_paged_create", "sals_paged_prepare", "sals_paged_destroy",
+    "sals_paged_append", "sals_paged_attend", "sals_paged_evict",
 )
 N_KERNELS = 9
 
@@ -42,6 +44,11 @@ class SalsDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "S_max", "H_q", "H_kv", "d", "r", "r_score", "top_k", "n_recent", "n_sink")] + \
                [("rope_theta", ctypes.c_float), ("rope_style", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class SalsPagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H_q", "H_kv", "d", "page_size", "max_pages", "n_pages", "weight_heads")] + \
+               [("page_stride", ctypes.c_int64), ("rope_theta", ctypes.c_float), ("rope_style", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class SalsError(RuntimeError):
@@ -93,6 +100,15 @@ def load_library() -> ctypes.CDLL:
     lib.sals_calib_eigenvectors_workspace_bytes.argtypes = [ctypes.c_int32]
     lib.sals_calib_eigenvectors.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp, vp,
                                             ctypes.c_size_t, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32), vp]
+    lib.sals_paged_workspace_bytes.argtypes = [ctypes.POINTER(SalsPagedDesc), ctypes.POINTER(ctypes.c_size_t)]
+    lib.sals_paged_create.argtypes = [ctypes.POINTER(SalsPagedDesc), vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+    lib.sals_paged_prepare.argtypes = [vp, vp]
+    lib.sals_paged_destroy.argtypes = [vp]
+    lib.sals_paged_destroy.restype = None
+    lib.sals_paged_append.argtypes = [vp, vp, vp, i32p, i32p, vp, vp, i32p, i32p, ctypes.c_int32, i32p, f32p, vp]
+    lib.sals_paged_attend.argtypes = [vp, vp, i32p, i32p, vp, vp, i32p, f32p, vp, vp]
+    lib.sals_paged_evict.argtypes = [vp, i32p, i32p, vp, vp, i32p, i32p, f32p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                     i32p, vp]
     lib.sals_kernel_name.restype = ctypes.c_char_p
     lib.sals_kernel_name.argtypes = [ctypes.c_int]
     lib.sals_profile_enable.argtypes = [vp, ctypes.c_int]
@@ -100,7 +116,7 @@ def load_library() -> ctypes.CDLL:
     for name in EXPORTS[1:]:
         if name.endswith("_workspace_bytes") and name.startswith("sals_calib"):
             getattr(lib, name).restype = ctypes.c_size_t
-        elif name not in ("sals_destroy", "sals_kernel_name"):
+        elif name not in ("sals_destroy", "sals_paged_destroy", "sals_kernel_name"):
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -132,6 +148,20 @@ def packed_weight_bytes(desc: SalsDesc) -> int:
     st = _lib.sals_packed_weight_bytes(ctypes.byref(desc), ctypes.byref(n))
     if st != SALS_OK:
         raise SalsError(st, "sals_packed_weight_bytes")
+    return int(n.value)
+
+
+def make_paged_desc(B, H_q, H_kv, d, page_size, max_pages, n_pages, dtype, weight_heads=0, page_stride=0, rope_theta=10000.0,
+                    rope_style=0) -> SalsPagedDesc:
+    dt = {"bf16": SALS_BF16, "f32": SALS_F32, torch.bfloat16: SALS_BF16, torch.float32: SALS_F32}[dtype]
+    return SalsPagedDesc(B, H_q, H_kv, d, page_size, max_pages, n_pages, weight_heads, page_stride, rope_theta, rope_style, dt)
+
+
+def paged_workspace_bytes(desc: SalsPagedDesc) -> int:
+    n = ctypes.c_size_t(0)
+    st = _lib.sals_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(n))
+    if st != SALS_OK:
+        raise SalsError(st, "sals_paged_workspace_bytes")
     return int(n.value)
 
 
@@ -338,3 +368,102 @@ class Sals:
     def overlap_score(self, q, q_pos, K, seq_len, idx, n_sel, os):
         self._check(_lib.sals_overlap_score(self._h, _p(q), _p(q_pos), _p(K), _p(seq_len), _p(idx), _p(n_sel),
                                             _p(os), _stream()), "sals_overlap_score")
+
+
+class Paged:
+    """One context of the paged key-value cache (include/sals.h): descriptor + caller-owned (torch) workspace.
+
+    Kp, Vp: pools [n_pages, page_size, H_kv, d] (dense pages, page_stride elements apart); table [B, max_pages] int32;
+    seq_len, q_pos [B] int32; with weight_heads > 0 pos int32 and weights fp32, both [B, weight_heads, max_pages * page_size].
+    The calls check types, sizes, layout and device of what they are given and raise SalsError; they run on the current stream."""
+
+    def __init__(self, desc: SalsPagedDesc, device="cuda:0"):
+        self.desc = desc
+        self.device = torch.device(device)
+        nbytes = paged_workspace_bytes(desc)
+        self._dtype = torch.bfloat16 if desc.dtype == SALS_BF16 else torch.float32
+        self._capacity = desc.page_size * desc.max_pages
+        self._row = desc.H_kv * desc.d
+        self._page_stride = desc.page_stride or desc.page_size * self._row
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self._index = self.workspace.get_device()
+        h = ctypes.c_void_p()
+        self._check(_lib.sals_paged_create(ctypes.byref(desc), self.workspace.data_ptr(), nbytes, ctypes.byref(h)), "sals_paged_create")
+        self._h = h
+        self._destroy = _lib.sals_paged_destroy   # kept on the instance: module globals may be gone at interpreter exit
+        with torch.cuda.device(self.device):
+            self._check(_lib.sals_paged_prepare(h, _stream()), "sals_paged_prepare")
+
+    def close(self):
+        h, self._h = getattr(self, "_h", None), None
+        destroy = getattr(self, "_destroy", None)
+        if h and destroy is not None:
+            destroy(h)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:   # interpreter shutdown: the library may already be unloaded
+            pass
+
+    @staticmethod
+    def _check(st, where):
+        if st != SALS_OK:
+            raise SalsError(st, where)
+
+    def _take(self, where, name, t, dtype, n):
+        """Device pointer of a dense tensor of n elements."""
+        if t.dtype is not dtype or t.numel() != n or t.get_device() != self._index or not t.is_contiguous():
+            raise SalsError(SALS_ERR_INVALID_ARG, f"{where}: {name} must be {n} dense elements of {dtype} on cuda:{self._index}")
+        return t.data_ptr()
+
+    def _pool(self, where, name, t):
+        d = self.desc
+        ok = t.dtype is self._dtype and t.get_device() == self._index and t.dim() == 4 and t.shape[0] >= d.n_pages and \
+            t.shape[1:] == (d.page_size, d.H_kv, d.d)
+        if ok:
+            s = t.stride()
+            ok = s[3] == 1 and (s[2] == d.d or d.H_kv == 1) and (s[1] == self._row or d.page_size == 1) and \
+                (s[0] == self._page_stride or d.n_pages == 1)
+        if not ok:
+            raise SalsError(SALS_ERR_INVALID_ARG, f"{where}: {name} must be a pool [{d.n_pages}, {d.page_size}, {d.H_kv}, {d.d}] of "
+                                                  f"{self._dtype} with {self._page_stride} elements from page to page on cuda:{self._index}")
+        return t.data_ptr()
+
+    def _common(self, where, q_pos, table, Kp, Vp, seq_len):
+        if self._h is None or torch.cuda.current_device() != self._index:
+            raise SalsError(SALS_ERR_INVALID_ARG, f"{where}: closed, or cuda:{self._index} is not the current device")
+        d = self.desc
+        return (self._take(where, "q_pos", q_pos, torch.int32, d.B), self._take(where, "table", table, torch.int32, d.B * d.max_pages),
+                self._pool(where, "Kp", Kp), self._pool(where, "Vp", Vp), self._take(where, "seq_len", seq_len, torch.int32, d.B))
+
+    def _lists(self, where, name, t, dtype):
+        d = self.desc
+        return None if t is None else self._take(where, name, t, dtype, d.B * d.weight_heads * self._capacity)
+
+    def append(self, k_new, v_new, q_pos, table, Kp, Vp, seq_len, n_tok=1, n_new=None, pos=None, weights=None):
+        """n_tok new tokens per sequence (k_new, v_new [B, n_tok, H_kv, d]; n_new [B] int32 of them count) from position q_pos on."""
+        w = "sals_paged_append"
+        qp, tb, kp, vp, sl = self._common(w, q_pos, table, Kp, Vp, seq_len)
+        n = self.desc.B * int(n_tok) * self._row
+        self._check(_lib.sals_paged_append(
+            self._h, self._take(w, "k_new", k_new, self._dtype, n), self._take(w, "v_new", v_new, self._dtype, n), qp, tb, kp, vp, sl,
+            None if n_new is None else self._take(w, "n_new", n_new, torch.int32, self.desc.B), int(n_tok),
+            self._lists(w, "pos", pos, torch.int32), self._lists(w, "weights", weights, torch.float32), _stream()), w)
+
+    def attend(self, q, q_pos, table, Kp, Vp, seq_len, out, weights=None):
+        """One new token per sequence (q, out [B, H_q, d]) over its cached slots; its softmax weights are added to `weights`."""
+        w, n = "sals_paged_attend", self.desc.B * self.desc.H_q * self.desc.d
+        qp, tb, kp, vp, sl = self._common(w, q_pos, table, Kp, Vp, seq_len)
+        self._check(_lib.sals_paged_attend(self._h, self._take(w, "q", q, self._dtype, n), qp, tb, kp, vp, sl,
+                                           self._lists(w, "weights", weights, torch.float32), self._take(w, "out", out, self._dtype, n),
+                                           _stream()), w)
+
+    def evict(self, q_pos, table, Kp, Vp, seq_len, pos, weights, n_keep, n_sink=0, n_recent=0, src=None):
+        """Sequences longer than n_keep keep n_keep slots of every list; src [B, weight_heads, n_keep] int32: where each came from."""
+        w = "sals_paged_evict"
+        qp, tb, kp, vp, sl = self._common(w, q_pos, table, Kp, Vp, seq_len)
+        self._check(_lib.sals_paged_evict(
+            self._h, qp, tb, kp, vp, sl, self._lists(w, "pos", pos, torch.int32), self._lists(w, "weights", weights, torch.float32),
+            int(n_keep), int(n_sink), int(n_recent),
+            None if src is None else self._take(w, "src", src, torch.int32, self.desc.B * self.desc.weight_heads * int(n_keep)), _stream()), w)

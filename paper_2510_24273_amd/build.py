@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -42,10 +43,19 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + os.environ.get("SALS_EXTRA_FLAGS", "").split() + ["-o", LIB] + sources()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    flags = HIPCC_FLAGS + os.environ.get("SALS_EXTRA_FLAGS", "").split()
+    with tempfile.TemporaryDirectory() as tmp:   # the sources side by side, then one link in the order of their names
+        jobs, objs = [], []
+        for src in sources():
+            objs.append(os.path.join(tmp, os.path.basename(src) + ".o"))
+            cmd = [hipcc] + [f for f in flags if f != "-shared"] + ["-c", src, "-o", objs[-1]]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((cmd, subprocess.Popen(cmd)))
+        failed = [(cmd, p.returncode) for cmd, p in jobs if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(failed[0][1], failed[0][0])
+        subprocess.run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs, check=True)
     return LIB
 
 
