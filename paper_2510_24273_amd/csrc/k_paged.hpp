@@ -122,108 +122,431 @@ __global__ __launch_bounds__(256) void paged_advance_kernel(int32_t* seq_len, co
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------
-// Logits are kept in units of ln 2 (the query is scaled by log2(e) / sqrt(D)), so that exponentials are powers of two.
+// softmax over a sequence's slots in one pass over K and V, the work split over the slots of the whole batch.
+//
+// Work.  A sequence of S slots is ceil(S / TB) blocks of TB slots (at least one, so that somebody writes its output); the blocks of
+// all sequences, one behind the other, are dealt in equal consecutive shares to the workgroups of a KV head.  A share may begin and
+// end inside a sequence and hold whole ones, so a ragged batch loads the chip as evenly as an even one.  What a workgroup finds of a
+// sequence that others share goes to the workspace, and the last of them to arrive joins the pieces in the order of the shares.
+//
+// Matrix cores.  A wave takes a block at a time, for up to 16 query heads of a KV head (the columns):
+//   S^T = K q^T      rows = slots, contraction over channels: a lane's 16 bytes of a K row are an operand as they lie in memory
+//   O^T += V^T p^T   rows = channels, contraction over slots: the lane that holds the weights of slots c CH .. c CH + CH - 1 of head n
+//                    (the layout that S^T leaves, with the slots of K's rows dealt accordingly) needs the same slots of channel n of V;
+//                    it loads 16 (8) bytes of each of their rows and byte permutes turn them, so nothing passes through LDS.
+// bf16: the rotated query is three bf16 pieces (exact to fp32's own rounding), a weight a head cut off and a remainder (2^-14 of it
+// lost at most), products and sums fp32.  The remainder is never zero beside a nonzero head: an infinite value stays one.
+// A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
+constexpr int kPgWaves = 8;
+constexpr int kPgJoin = 4;             // copies of the output that a workgroup's waves are added up in
 
-// grid (chunks, H_kv * head tiles, B): a wave takes a token at a time, a lane D / 64 channels of it
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_attend_kernel(PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
-                                                           const T* __restrict__ Kp, const T* __restrict__ Vp, float* __restrict__ part,
-                                                           float* __restrict__ logits, float scale, double log2_theta, int style)
+template <typename T> struct PgBlock;
+template <> struct PgBlock<bf16_t> { static constexpr int TB = 32; };
+template <> struct PgBlock<float> { static constexpr int TB = 16; };
+
+struct PagedWork {
+    int blocks, shares, q, r;     // of all sequences; workgroups of a head; the first r shares have q + 1 blocks, the others q
+    __device__ __forceinline__ int begin(int w) const { return w * q + min(w, r); }
+    __device__ __forceinline__ int share(int x) const   // the one that block x belongs to
+    {
+        const uint32_t split = (uint32_t)r * (uint32_t)(q + 1);
+        return (uint32_t)x < split ? (int)((uint32_t)x / (uint32_t)(q + 1)) : r + (int)(((uint32_t)x - split) / (uint32_t)q);
+    }
+};
+
+struct PagedParts {               // pieces of shared sequences: slot 2 w of share w for one that began before it, 2 w + 1 for one that goes on behind
+    float* sum;                   // [2 shares][heads of the grid][rows][D]
+    float2* stat;                 // [2 shares][heads of the grid][rows]
+    uint32_t* count;              // [B][heads of the grid]
+    float2* final_stat;           // [B * H]: maximum, 1 / sum
+    int rows;                     // query heads of a workgroup at most
+};
+
+__device__ __forceinline__ float max_xor_rows(float v)   // over the four lanes that hold a head
 {
-    constexpr int CPL = D / 64, REC = D + 2;
-    __shared__ float sQ[kPgHeads][D];
-    __shared__ float2 sCS[D / 2];
-    __shared__ float sRed[4][REC];
-    const int chunk = blockIdx.x, n_chunks = gridDim.x, b = blockIdx.z;
-    const int tiles = (a.group + kPgHeads - 1) / kPgHeads, g = blockIdx.y / tiles, h0 = blockIdx.y % tiles * kPgHeads;
-    const int nh = min(kPgHeads, a.group - h0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int H = a.H_kv * a.group;
-    const int S = min(max(a.seq_len[b], 0), a.cap);
-    const int per = ((S + n_chunks - 1) / n_chunks + 3) & ~3, j0 = min(S, chunk * per), j1 = min(S, j0 + per);
-    if (tid < D / 2) sCS[tid] = rope_turn<D>(q_pos[b], tid, log2_theta);
-    __syncthreads();
-    for (int i = tid; i < nh * (D / 2); i += 256) {
-        const int m = i / (D / 2), p = i % (D / 2), c1 = pair_lo<D>(p, style), c2 = pair_hi<D>(p, style);
-        const T* qh = q + ((size_t)b * H + (size_t)g * a.group + h0 + m) * D;
-        const float x = elem<T>::load(qh + c1), y = elem<T>::load(qh + c2);
-        sQ[m][c1] = (x * sCS[p].x - y * sCS[p].y) * scale;
-        sQ[m][c2] = (y * sCS[p].x + x * sCS[p].y) * scale;
-    }
-    __syncthreads();
-    float mx[kPgHeads], l[kPgHeads], acc[kPgHeads][CPL];
-#pragma unroll
-    for (int m = 0; m < kPgHeads; ++m) {
-        mx[m] = -INFINITY; l[m] = 0.f;
-        for (int c = 0; c < CPL; ++c) acc[m][c] = 0.f;
-    }
-    const int row = a.H_kv * D;
-    for (int j = j0 + wave; j < j1; j += 4) {
-        const int64_t at = paged_row(a, b, j, row);
-        float k[CPL], v[CPL];
-        if (at >= 0)
-            for (int c = 0; c < CPL; ++c) {
-                k[c] = elem<T>::load(Kp + at + g * D + lane * CPL + c);
-                v[c] = elem<T>::load(Vp + at + g * D + lane * CPL + c);
-            }
-#pragma unroll
-        for (int m = 0; m < kPgHeads; ++m) {
-            if (m >= nh) continue;
-            float x = -INFINITY;
-            if (at >= 0) {
-                x = 0.f;
-                for (int c = 0; c < CPL; ++c) x = fmaf(sQ[m][lane * CPL + c], k[c], x);
-                x = wave_sum(x);
-                const float mn = fmaxf(mx[m], x), r = exp2f(mx[m] - mn), p = exp2f(x - mn);
-                mx[m] = mn;
-                l[m] = l[m] * r + p;
-                for (int c = 0; c < CPL; ++c) acc[m][c] = fmaf(p, v[c], acc[m][c] * r);
-            }
-            if (logits && lane == 0) logits[((size_t)b * H + (size_t)g * a.group + h0 + m) * a.cap + j] = x;
-        }
-    }
-    for (int m = 0; m < kPgHeads; ++m) {
-        if (m >= nh) break;
-        __syncthreads();
-        if (lane == 0) { sRed[wave][0] = mx[m]; sRed[wave][1] = l[m]; }
-        for (int c = 0; c < CPL; ++c) sRed[wave][2 + lane * CPL + c] = acc[m][c];
-        __syncthreads();
-        if (tid < D) {
-            float M = -INFINITY, L = 0.f, A = 0.f;
-            for (int w = 0; w < 4; ++w) M = fmaxf(M, sRed[w][0]);
-            for (int w = 0; w < 4 && M > -INFINITY; ++w) {
-                const float f = exp2f(sRed[w][0] - M);
-                L = fmaf(sRed[w][1], f, L);
-                A = fmaf(sRed[w][2 + tid], f, A);
-            }
-            float* rec = part + (((size_t)b * H + (size_t)g * a.group + h0 + m) * n_chunks + chunk) * REC;
-            if (tid == 0) { rec[0] = M; rec[1] = L; }
-            rec[2 + tid] = A;
-        }
-    }
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float sum_xor_rows(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
 }
 
-// grid (B * H): the chunks joined; (maximum, 1 / sum) left for the weights
-template <typename T, int D>
-__global__ __launch_bounds__(D) void paged_merge_kernel(const float* __restrict__ part, T* __restrict__ out, float2* __restrict__ stat, int n_chunks)
+// grid (shares * H_kv * head tiles); logits: null, or [B * H][logit_stride] to be left
+template <typename T, int D, bool WHOLE>   // WHOLE: the CH slots of a lane lie in one page
+__global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
+                                                                       const T* __restrict__ Kp, const T* __restrict__ Vp, T* __restrict__ out,
+                                                                       PagedParts parts, float* __restrict__ logits, int logit_stride, int max_shares,
+                                                                       int least, float scale, double log2_theta, int style)
 {
-    const size_t bh = blockIdx.x;
-    const float* rec = part + bh * n_chunks * (D + 2);
-    float M = -INFINITY, L = 0.f, A = 0.f;
-    for (int k = 0; k < n_chunks; ++k) M = fmaxf(M, rec[(size_t)k * (D + 2)]);
-    for (int k = 0; k < n_chunks && M > -INFINITY; ++k) {
-        const float* r = rec + (size_t)k * (D + 2);
-        const float f = exp2f(r[0] - M);
-        L = fmaf(r[1], f, L);
-        A = fmaf(r[2 + threadIdx.x], f, A);
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int TB = PgBlock<T>::TB, CH = TB / 4, VEC = elem<T>::vec;
+    constexpr int NKT = TB / 16;               // row tiles of S^T
+    constexpr int NS = D / (4 * VEC);          // 16-byte pieces of a K row per lane
+    constexpr int NJ = D / 16;                 // row tiles of O^T
+    constexpr int VW = NJ * sizeof(T) / 4;     // 32-bit words of a V row per lane
+    constexpr int NID = WHOLE ? 1 : CH, NIK = WHOLE ? 1 : NKT;
+    constexpr int LROW = D + 4;
+    __shared__ float2 sCS[D / 2];
+    __shared__ float sM[kPgWaves][kPgHeads], sL[kPgWaves][kPgHeads];
+    __shared__ __attribute__((aligned(16))) float sO[kPgJoin][kPgHeads][LROW];
+    __shared__ uint32_t sLast;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6), n16 = lane & 15, c4 = lane >> 4;
+    const int tiles = (a.group + kPgHeads - 1) / kPgHeads, heads = a.H_kv * tiles, H = a.H_kv * a.group;
+    const int w = blockIdx.x / heads, hg = blockIdx.x - w * heads, g = hg / tiles, h0 = g * a.group + (hg - g * tiles) * kPgHeads;
+    const int nh = min(kPgHeads, (g + 1) * a.group - h0);
+    const int row = a.H_kv * D;
+
+    // ---- this workgroup's share ----
+    const int per = (a.B + 63) >> 6;           // sequences of a lane
+    auto blocks_of = [&](int b) { return max(1, (min(max(a.seq_len[b], 0), a.cap) + TB - 1) / TB); };
+    uint32_t mine = 0;
+    for (int i = 0; i < per; ++i) mine += lane * per + i < a.B ? (uint32_t)blocks_of(lane * per + i) : 0u;
+    const uint32_t upto = wave_incl_scan(mine);
+    PagedWork W;
+    W.blocks = __builtin_amdgcn_readlane((int)upto, 63);
+    W.shares = max(1, min(max_shares, W.blocks / least));
+    if (w >= W.shares) return;
+    W.q = W.blocks / W.shares;
+    W.r = W.blocks - W.q * W.shares;
+    int at = W.begin(w);
+    const int end = W.begin(w + 1);
+    const int first_lane = __popcll(__ballot(upto <= (uint32_t)at));
+    int b = first_lane * per, base = __builtin_amdgcn_readlane((int)(upto - mine), first_lane);
+    for (int n; base + (n = wave_uniform(blocks_of(b))) <= at; ++b) base += n;
+
+    while (at < end) {
+        const int S = wave_uniform(min(max(a.seq_len[b], 0), a.cap)), n_blocks = max(1, (S + TB - 1) / TB);
+        const int blk0 = at - base, blk1 = min(end - base, n_blocks), live1 = min(blk1, (S + TB - 1) / TB);
+        const int32_t* tb = a.table + (size_t)b * a.max_pages;
+
+        // ---- pages and rows of a block ----
+        struct Ids { int32_t k[NIK], v[NID]; };
+        auto k_slot = [&](int t0, int t) { return WHOLE ? t0 + (n16 >> 2) * CH : min(t0 + (n16 >> 2) * CH + t * 4 + (n16 & 3), S - 1); };
+        auto v_slot = [&](int t0, int e) { return WHOLE ? t0 + c4 * CH : min(t0 + c4 * CH + e, S - 1); };
+        // a run of CH slots that begins past the end re-reads the last one that does not
+        auto held = [&](int j) { return WHOLE ? min(j, (S - 1) & ~(CH - 1)) : j; };
+        auto load_ids = [&](Ids& I, int blk) {
+            const int t0 = min(blk, live1 - 1) * TB;
+#pragma unroll
+            for (int t = 0; t < NIK; ++t) I.k[t] = tb[page_of((uint32_t)held(k_slot(t0, t)), a.page_mul)];
+#pragma unroll
+            for (int e = 0; e < NID; ++e) I.v[e] = tb[page_of((uint32_t)held(v_slot(t0, e)), a.page_mul)];
+        };
+        // element offset of slot j's row; a page that is not there is read as page 0, and masked
+        auto row_at = [&](int32_t id, int j) {
+            const uint32_t pg = page_of((uint32_t)j, a.page_mul);
+            const uint32_t page = (uint32_t)id < (uint32_t)a.n_pages ? (uint32_t)id : 0u;
+            return (int64_t)page * a.page_stride + (int64_t)(uint32_t)((j - (int)pg * a.page_size) * row);
+        };
+        u32x4 K[NKT][NS];
+        uint32_t V[CH][VW];
+        auto load_k = [&](const Ids& I, int blk) {
+            const int t0 = blk * TB;
+#pragma unroll
+            for (int t = 0; t < NKT; ++t) {
+                const int j = held(k_slot(t0, t));
+                const T* p = Kp + row_at(I.k[WHOLE ? 0 : t], j) + (WHOLE ? (t * 4 + (n16 & 3)) * row : 0) + g * D + c4 * VEC;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) K[t][s] = ld16_stream(p + s * 4 * VEC);
+            }
+        };
+        auto load_v = [&](const Ids& I, int blk) {
+            const int t0 = blk * TB;
+            const T* p0 = nullptr;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                if (!WHOLE || e == 0) p0 = Vp + row_at(I.v[WHOLE ? 0 : e], held(v_slot(t0, e))) + g * D;
+                const T* p = WHOLE ? p0 + e * row : p0;
+                if constexpr (BF && VW == 2) {
+                    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + n16 * NJ));
+                    V[e][0] = x.x; V[e][1] = x.y;
+                } else {
+#pragma unroll
+                    for (int h = 0; h < VW / 4; ++h) {   // fp32: pieces of 4 channels, 64 channels apart
+                        const u32x4 x = ld16_stream(p + h * 64 + n16 * VEC);
+                        V[e][4 * h] = x.x; V[e][4 * h + 1] = x.y; V[e][4 * h + 2] = x.z; V[e][4 * h + 3] = x.w;
+                    }
+                }
+            }
+        };
+
+        // the first loads wait for the length and the table only
+        int blk = blk0 + wave;
+        Ids I0, I1;
+        if (blk < live1) {
+            load_ids(I0, blk);
+            load_ids(I1, blk + kPgWaves);
+            load_k(I0, blk);
+            load_v(I0, blk);
+        }
+
+        // ---- the rotated query of these heads, scaled ----
+        const bool has = n16 < nh;
+        u32x4 qraw[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            qraw[s] = u32x4{0u, 0u, 0u, 0u};
+            if (has) qraw[s] = ld16(q + ((size_t)b * H + h0 + n16) * D + s * 4 * VEC + c4 * VEC);
+        }
+        if (tid < D / 2) sCS[tid] = rope_turn<D>(q_pos[b], tid, log2_theta);
+        __syncthreads();
+        float qf[NS][VEC];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) elem<T>::unpack(qraw[s], qf[s]);
+        if (style) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const float2 cs = sCS[(s * 4 * VEC + c4 * VEC + e) / 2];
+                    const float x = qf[s][e], y = qf[s][e + 1];
+                    qf[s][e] = fmaf(x, cs.x, -(y * cs.y)) * scale;
+                    qf[s][e + 1] = fmaf(y, cs.x, x * cs.y) * scale;
+                }
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS / 2; ++s)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float2 cs = sCS[s * 4 * VEC + c4 * VEC + e];
+                    const float x = qf[s][e], y = qf[s + NS / 2][e];
+                    qf[s][e] = fmaf(x, cs.x, -(y * cs.y)) * scale;
+                    qf[s + NS / 2][e] = fmaf(y, cs.x, x * cs.y) * scale;
+                }
+        }
+        u32x4 qp[BF ? 3 : 1][NS];
+        if constexpr (BF) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t lo = f32_to_bf16(qf[s][2 * e]), hi = f32_to_bf16(qf[s][2 * e + 1]);
+                        qf[s][2 * e] -= bf16_to_f32((bf16_t)lo);
+                        qf[s][2 * e + 1] -= bf16_to_f32((bf16_t)hi);
+                        qp[k][s][e] = lo | hi << 16;
+                    }
+        }
+
+        // ---- the stream ----
+        float m = -INFINITY, l = 0.f;
+        f32x4 O[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (; blk < live1; blk += kPgWaves) {
+            const int t0 = blk * TB;
+            const bool more = blk + kPgWaves < live1;
+            f32x4 x[NKT];
+#pragma unroll
+            for (int t = 0; t < NKT; ++t) {
+                x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    if constexpr (BF) {
+#pragma unroll
+                        for (int k = 2; k >= 0; --k)
+                            x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, K[t][s]), __builtin_bit_cast(bf16x8, qp[k][s]), x[t], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(K[t][s][e]), qf[s][e], x[t], 0, 0, 0);
+                    }
+                }
+            }
+            // which of this lane's slots count (slot t0 + CH c4 + e is x[e / 4][e % 4])
+            bool whole = t0 + TB <= S;
+#pragma unroll
+            for (int e = 0; e < NID; ++e) whole = whole && (uint32_t)I0.v[e] < (uint32_t)a.n_pages;
+            if (__ballot(!whole)) {
+#pragma unroll
+                for (int e = 0; e < CH; ++e) {
+                    const bool ok = t0 + c4 * CH + e < S && (uint32_t)I0.v[WHOLE ? 0 : e] < (uint32_t)a.n_pages;
+                    if (!ok) x[e >> 2][e & 3] = -INFINITY;
+                }
+            }
+            const uint64_t part_of = __ballot(!whole);
+            Ids I2;
+            if (more) {
+                load_ids(I2, blk + 2 * kPgWaves);
+                load_k(I1, blk + kPgWaves);
+            }
+            if (logits && has) {
+                float* to = logits + (size_t)((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
+#pragma unroll
+                for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = x[t];
+            }
+            float top = x[0][0];
+#pragma unroll
+            for (int e = 1; e < CH; ++e) top = fmaxf(top, x[e >> 2][e & 3]);
+            if (__ballot(top > m + 8.f)) {   // (also the first time: m is -infinity)
+                const float mn = fmaxf(m, max_xor_rows(top));
+                const float f = mn > -INFINITY ? __builtin_amdgcn_exp2f(m - mn) : 1.f;
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) O[j] *= f;
+            }
+            const float ref = m > -INFINITY ? m : 0.f;   // (nothing yet: all are -infinity)
+            float p[CH];
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(x[e >> 2][e & 3] - ref);
+                l += p[e];
+            }
+            if (part_of) {   // what lies in slots that do not count may be anything
+#pragma unroll
+                for (int e = 0; e < CH; ++e) {
+                    const bool ok = t0 + c4 * CH + e < S && (uint32_t)I0.v[WHOLE ? 0 : e] < (uint32_t)a.n_pages;
+#pragma unroll
+                    for (int k = 0; k < VW; ++k) V[e][k] = ok ? V[e][k] : 0u;
+                }
+            }
+            if constexpr (BF) {
+                u32x4 ph, pl;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t u0 = __float_as_uint(p[2 * k]), u1 = __float_as_uint(p[2 * k + 1]);
+                    ph[k] = __builtin_amdgcn_perm(u1, u0, 0x07060302);
+                    const float r0 = fmaxf(p[2 * k] - __uint_as_float(u0 & 0xffff0000u), p[2 * k] * 0x1p-20f);
+                    const float r1 = fmaxf(p[2 * k + 1] - __uint_as_float(u1 & 0xffff0000u), p[2 * k + 1] * 0x1p-20f);
+                    pl[k] = (uint32_t)f32_to_bf16(r0) | (uint32_t)f32_to_bf16(r1) << 16;
+                }
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    u32x4 v;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_perm(V[2 * k + 1][j >> 1], V[2 * k][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
+                    O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pl), O[j], 0, 0, 0);
+                    O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, ph), O[j], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(V[e][j]), p[e], O[j], 0, 0, 0);
+            }
+            if (more) load_v(I1, blk + kPgWaves);
+            I0 = I1;
+            I1 = I2;
+        }
+
+        // ---- the waves joined ----
+        l = sum_xor_rows(l);
+        if (lane < kPgHeads) { sM[wave][lane] = m; sL[wave][lane] = l; }
+        __syncthreads();
+        float M = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < kPgWaves; ++v) M = fmaxf(M, sM[v][n16]);
+        const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - M) : 0.f;
+        // channel of O[j][i] of this lane
+        auto channel = [&](int j, int i) { return BF ? (c4 * 4 + i) * NJ + j : (j >> 2) * 64 + (c4 * 4 + i) * 4 + (j & 3); };
+        auto put = [&](int at_copy) {
+            if (!has) return;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; j += 4)
+                    *reinterpret_cast<f32x4*>(&sO[at_copy][n16][channel(j, i)]) = f32x4{O[j][i] * f, O[j + 1][i] * f, O[j + 2][i] * f, O[j + 3][i] * f};
+        };
+        auto add = [&](int at_copy) {
+            if (!has) return;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; j += 4) {
+                    f32x4* to = reinterpret_cast<f32x4*>(&sO[at_copy][n16][channel(j, i)]);
+                    *to += f32x4{O[j][i] * f, O[j + 1][i] * f, O[j + 2][i] * f, O[j + 3][i] * f};
+                }
+        };
+        if (wave < kPgJoin) put(wave);
+        __syncthreads();
+        if (wave >= kPgJoin) add(wave - kPgJoin);
+        __syncthreads();
+        const bool alone = blk0 == 0 && blk1 == n_blocks;
+        const int w0 = W.share(base), w1 = W.share(base + n_blocks - 1);   // the shares that this sequence is spread over
+        // M and the normaliser of head h (of the tile)
+        auto norm = [&](int h, float* Mh) {
+            float Mx = -INFINITY, L = 0.f;
+            for (int v = 0; v < kPgWaves; ++v) Mx = fmaxf(Mx, sM[v][h]);
+            for (int v = 0; v < kPgWaves; ++v) L += sM[v][h] > -INFINITY ? sL[v][h] * __builtin_amdgcn_exp2f(sM[v][h] - Mx) : 0.f;
+            *Mh = Mx;
+            return L;
+        };
+        const size_t piece = ((size_t)(2 * w + (blk0 == 0)) * heads + hg) * parts.rows;
+        for (int i = tid; i < nh * D; i += kPgWaves * 64) {
+            const int h = i / D, ch = i % D;
+            float Mh;
+            const float L = norm(h, &Mh);
+            const float A = (sO[0][h][ch] + sO[1][h][ch]) + (sO[2][h][ch] + sO[3][h][ch]);
+            if (alone) {
+                elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
+                if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mh : 0.f, L != 0.f ? 1.f / L : 0.f);
+            } else {
+                parts.sum[(piece + h) * D + ch] = A;
+                if (ch == 0) parts.stat[piece + h] = make_float2(Mh, L);
+            }
+        }
+        if (!alone) {
+            // the pieces are visible to the device before this workgroup counts as arrived, and the others' to the last one to arrive
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                sLast = arrive(parts.count + (size_t)b * heads + hg, (uint32_t)(w1 - w0 + 1)) == (uint32_t)(w1 - w0);
+                __threadfence();
+            }
+            __syncthreads();
+            if (sLast) {
+                __threadfence();
+                // [(share, kind)] of the pieces: the first share's goes on behind it, the others' began before
+                auto piece_of = [&](int v) { return ((size_t)(2 * v + (v == w0)) * heads + hg) * parts.rows; };
+                for (int i = tid; i < nh * D; i += kPgWaves * 64) {
+                    const int h = i / D, ch = i % D;
+                    float Mx = -INFINITY, L = 0.f, A = 0.f;
+                    for (int v = w0; v <= w1; v += 8) {
+                        float2 st[8];
+                        float s[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const size_t pc = piece_of(min(v + u, w1)) + h;
+                            st[u] = parts.stat[pc];
+                            s[u] = parts.sum[pc * D + ch];
+                        }
+                        float mn = Mx;
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) mn = fmaxf(mn, st[u].x);
+                        if (mn > -INFINITY) {
+                            const float f0 = __builtin_amdgcn_exp2f(Mx - mn);
+                            L *= f0;
+                            A *= f0;
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const float fu = v + u <= w1 && st[u].x > -INFINITY ? __builtin_amdgcn_exp2f(st[u].x - mn) : 0.f;
+                                L = fmaf(st[u].y, fu, L);
+                                A = fu != 0.f ? fmaf(s[u], fu, A) : A;
+                            }
+                            Mx = mn;
+                        }
+                    }
+                    elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
+                    if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mx : 0.f, L != 0.f ? 1.f / L : 0.f);
+                }
+            }
+        }
+        __syncthreads();   // (LDS is taken anew by the next sequence)
+        base += n_blocks;
+        at = base;
+        ++b;
     }
-    elem<T>::store(out + bh * D + threadIdx.x, L > 0.f ? A / L : 0.f);
-    if (threadIdx.x == 0) stat[bh] = make_float2(L > 0.f ? M : 0.f, L > 0.f ? 1.f / L : 0.f);
 }
 
 // weights[b, list, j] += sum over the list's heads of the softmax weight.  grid (x, lists, B)
 __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const float* __restrict__ logits, const float2* __restrict__ stat,
-                                                            float* __restrict__ weights)
+                                                            int logit_stride, float* __restrict__ weights)
 {
     const int lists = gridDim.y, b = blockIdx.z, H = a.H_kv * a.group, nh = H / lists, h0 = blockIdx.y * nh;
     const int S = min(max(a.seq_len[b], 0), a.cap);
@@ -232,7 +555,7 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
         float sum = 0.f;
         for (int h = 0; h < nh; ++h) {
             const float2 st = stat[(size_t)b * H + h0 + h];
-            sum += exp2f(logits[((size_t)b * H + h0 + h) * a.cap + j] - st.x) * st.y;
+            sum += exp2f(logits[((size_t)b * H + h0 + h) * logit_stride + j] - st.x) * st.y;
         }
         w[j] += sum;
     }

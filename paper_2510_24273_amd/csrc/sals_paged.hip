@@ -19,9 +19,12 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline bool bad(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SALS_OK : SALS_ERR_HIP; }
 
+constexpr int kPgGroups = 256;   // workgroups of the attention: one per compute unit
+constexpr int kPgLeast = 4;      // blocks of a share at least, as far as there are that many
+
 struct PagedLayout {  // byte offsets into the workspace
-    size_t count, part, stat, logits, moves, from, to, total;
-    int n_count, chunks, move_cap;
+    size_t count, sum, stat, final_stat, logits, moves, from, to, total;
+    int n_count, shares, rows, move_cap, logit_stride;
 };
 
 inline int capacity(const sals_paged_desc& d) { return d.max_pages * d.page_size; }
@@ -49,17 +52,23 @@ PagedLayout make_layout(const sals_paged_desc& d)
 {
     PagedLayout L{};
     const size_t H = (size_t)d.B * d.H_q, cap = (size_t)capacity(d);
-    L.n_count = d.B * d.H_kv * ceil_div(d.H_q / d.H_kv, kPgHeads);
-    L.chunks = std::max(1, std::min(32, ceil_div((int)cap, 256)));
+    const int group = d.H_q / d.H_kv, heads = d.H_kv * ceil_div(group, kPgHeads), tb = d.dtype == SALS_BF16 ? PgBlock<bf16_t>::TB : PgBlock<float>::TB;
+    L.n_count = d.B * heads;
+    // a workgroup per compute unit, no more than there can be blocks
+    L.shares = (int)std::max<int64_t>(1, std::min<int64_t>(kPgGroups / heads, (int64_t)d.B * ceil_div((int)cap, tb)));
+    L.rows = std::min(group, kPgHeads);
+    L.logit_stride = ceil_div((int)cap, 32) * 32;
     L.move_cap = (int)cap / 2 + 1;   // (no more than half of the slots can move below the others)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes); return r; };
     L.count = take((size_t)L.n_count * 4);
-    L.part = take(H * L.chunks * (d.d + 2) * 4);
-    L.stat = take(H * 8);
+    const size_t pieces = (size_t)2 * L.shares * heads * L.rows;
+    L.sum = take(pieces * d.d * 4);
+    L.stat = take(pieces * 8);
+    L.final_stat = take(H * 8);
     if (d.weight_heads) {
         const size_t rows = (size_t)d.B * d.weight_heads;
-        L.logits = take(H * cap * 4);
+        L.logits = take(H * L.logit_stride * 4);
         L.moves = take(rows * 4);
         L.from = take(rows * L.move_cap * 4);
         L.to = take(rows * L.move_cap * 4);
@@ -115,17 +124,21 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
 {
     const sals_paged_desc& d = c->d;
     const PagedCache a = cache_of(c, table, seq_len);
-    float* part = at<float>(c, c->L.part);
-    float* logits = weights ? at<float>(c, c->L.logits) : nullptr;
-    float2* stat = at<float2>(c, c->L.stat);
+    const PagedLayout& L = c->L;
+    float* logits = weights ? at<float>(c, L.logits) : nullptr;
+    const PagedParts parts{at<float>(c, L.sum), at<float2>(c, L.stat), at<uint32_t>(c, L.count), at<float2>(c, L.final_stat), L.rows};
     const float scale = (float)(1.4426950408889634074 / std::sqrt((double)D));
-    hipLaunchKernelGGL((paged_attend_kernel<T, D>), dim3(c->L.chunks, d.H_kv * ceil_div(a.group, kPgHeads), d.B), dim3(256), 0, st, a,
-                       static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), part, logits, scale, c->log2_theta,
-                       d.rope_style);
-    if (launch_status() != SALS_OK) return SALS_ERR_HIP;
-    hipLaunchKernelGGL((paged_merge_kernel<T, D>), dim3(d.B * d.H_q), dim3(D), 0, st, part, static_cast<T*>(out), stat, c->L.chunks);
+    const dim3 grid(L.shares * d.H_kv * ceil_div(a.group, kPgHeads));
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kPgWaves * 64), 0, st, a, static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp),
+                           static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits, L.logit_stride, L.shares, kPgLeast, scale, c->log2_theta,
+                           d.rope_style);
+    };
+    if (d.page_size % (PgBlock<T>::TB / 4) == 0) launch(paged_attend_kernel<T, D, true>);
+    else launch(paged_attend_kernel<T, D, false>);
     if (launch_status() != SALS_OK || !weights) return launch_status();
-    hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 256)), d.weight_heads, d.B), dim3(256), 0, st, a, logits, stat, weights);
+    hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 256)), d.weight_heads, d.B), dim3(256), 0, st, a, logits,
+                       at<float2>(c, L.final_stat), L.logit_stride, weights);
     return launch_status();
 }
 
