@@ -139,6 +139,8 @@ __global__ __launch_bounds__(256) void paged_advance_kernel(int32_t* seq_len, co
 // A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
 constexpr int kPgWaves = 8;
+constexpr int kPgGroups = 256;         // workgroups: one per compute unit
+constexpr int kPgAhead = 32;           // pieces of a shared sequence that a thread requests together
 constexpr int kPgJoin = 4;             // copies of the output that a workgroup's waves are added up in
 
 template <typename T> struct PgBlock;
@@ -162,6 +164,13 @@ struct PagedParts {               // pieces of shared sequences: slot 2 w of sha
     float2* final_stat;           // [B * H]: maximum, 1 / sum
     int rows;                     // query heads of a workgroup at most
 };
+
+// Stores and loads that pass the caches of the compute unit and of its die, for what one workgroup leaves to another of the same
+// launch: ordinary ones would need a write-back and an invalidation of a whole L2 around them.  A workgroup's stores
+// are done, for every workgroup of the device, behind device_stores_done() in every thread and a barrier.
+__device__ __forceinline__ void st_device(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float ld_device(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void device_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float max_xor_rows(float v)   // over the four lanes that hold a head
 {
@@ -192,6 +201,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
     __shared__ float2 sCS[D / 2];
     __shared__ float sM[kPgWaves][kPgHeads], sL[kPgWaves][kPgHeads];
     __shared__ __attribute__((aligned(16))) float sO[kPgJoin][kPgHeads][LROW];
+    __shared__ float sF[kPgHeads][kPgGroups];
     __shared__ uint32_t sLast;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6), n16 = lane & 15, c4 = lane >> 4;
@@ -487,53 +497,63 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
                 elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
                 if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mh : 0.f, L != 0.f ? 1.f / L : 0.f);
             } else {
-                parts.sum[(piece + h) * D + ch] = A;
-                if (ch == 0) parts.stat[piece + h] = make_float2(Mh, L);
+                st_device(parts.sum + (piece + h) * D + ch, A);
+                if (ch == 0) { st_device(&parts.stat[piece + h].x, Mh); st_device(&parts.stat[piece + h].y, L); }
             }
         }
         if (!alone) {
-            // the pieces are visible to the device before this workgroup counts as arrived, and the others' to the last one to arrive
-            __threadfence();
+            // the pieces are where the whole device sees them before this workgroup counts as arrived
+            device_stores_done();
             __syncthreads();
-            if (tid == 0) {
-                sLast = arrive(parts.count + (size_t)b * heads + hg, (uint32_t)(w1 - w0 + 1)) == (uint32_t)(w1 - w0);
-                __threadfence();
-            }
+            if (tid == 0) sLast = arrive(parts.count + (size_t)b * heads + hg, (uint32_t)(w1 - w0 + 1)) == (uint32_t)(w1 - w0);
             __syncthreads();
             if (sLast) {
-                __threadfence();
-                // [(share, kind)] of the pieces: the first share's goes on behind it, the others' began before
+                // (share, kind) of the pieces: the first share's goes on behind it, the others' began before
                 auto piece_of = [&](int v) { return ((size_t)(2 * v + (v == w0)) * heads + hg) * parts.rows; };
+                const int n = w1 - w0 + 1;
+                auto sums = [&](float (&x)[kPgAhead], int i, int v) {   // of column i = (head, channel), shares w0 + v ...
+#pragma unroll
+                    for (int u = 0; u < kPgAhead; ++u) x[u] = ld_device(parts.sum + piece_of(w0 + min(v + u, n - 1)) * D + i);
+                };
+                float x[kPgAhead];
+                sums(x, min(tid, nh * D - 1), 0);
+                for (int h = wave; h < nh; h += kPgWaves) {   // a wave takes a head's statistics
+                    float2 st[kPgGroups / 64];
+                    float Mx = -INFINITY, L = 0.f;
+#pragma unroll
+                    for (int u = 0; u < kPgGroups / 64; ++u) {
+                        st[u] = make_float2(-INFINITY, 0.f);
+                        if (lane + 64 * u < n) {
+                            const float2* p = parts.stat + piece_of(w0 + lane + 64 * u) + h;
+                            st[u] = make_float2(ld_device(&p->x), ld_device(&p->y));
+                        }
+                        Mx = fmaxf(Mx, st[u].x);
+                    }
+                    Mx = wave_max(Mx);
+#pragma unroll
+                    for (int u = 0; u < kPgGroups / 64; ++u) {
+                        const float fu = st[u].x > -INFINITY ? __builtin_amdgcn_exp2f(st[u].x - Mx) : 0.f;
+                        L = fmaf(st[u].y, fu, L);
+                        if (lane + 64 * u < n) sF[h][lane + 64 * u] = fu;
+                    }
+                    L = wave_sum(L);
+                    if (lane == 0) { sM[0][h] = Mx; sL[0][h] = L; }
+                }
+                __syncthreads();
                 for (int i = tid; i < nh * D; i += kPgWaves * 64) {
                     const int h = i / D, ch = i % D;
-                    float Mx = -INFINITY, L = 0.f, A = 0.f;
-                    for (int v = w0; v <= w1; v += 8) {
-                        float2 st[8];
-                        float s[8];
+                    float A = 0.f;
+                    for (int v = 0; v < n; v += kPgAhead) {
+                        if (v > 0 || i != tid) sums(x, i, v);
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const size_t pc = piece_of(min(v + u, w1)) + h;
-                            st[u] = parts.stat[pc];
-                            s[u] = parts.sum[pc * D + ch];
-                        }
-                        float mn = Mx;
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) mn = fmaxf(mn, st[u].x);
-                        if (mn > -INFINITY) {
-                            const float f0 = __builtin_amdgcn_exp2f(Mx - mn);
-                            L *= f0;
-                            A *= f0;
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                const float fu = v + u <= w1 && st[u].x > -INFINITY ? __builtin_amdgcn_exp2f(st[u].x - mn) : 0.f;
-                                L = fmaf(st[u].y, fu, L);
-                                A = fu != 0.f ? fmaf(s[u], fu, A) : A;
-                            }
-                            Mx = mn;
+                        for (int u = 0; u < kPgAhead; ++u) {
+                            const float fu = v + u < n ? sF[h][min(v + u, n - 1)] : 0.f;
+                            A = fu != 0.f ? fmaf(x[u], fu, A) : A;
                         }
                     }
+                    const float L = sL[0][h];
                     elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
-                    if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mx : 0.f, L != 0.f ? 1.f / L : 0.f);
+                    if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? sM[0][h] : 0.f, L != 0.f ? 1.f / L : 0.f);
                 }
             }
         }

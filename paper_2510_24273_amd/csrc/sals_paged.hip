@@ -19,7 +19,6 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline bool bad(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SALS_OK : SALS_ERR_HIP; }
 
-constexpr int kPgGroups = 256;   // workgroups of the attention: one per compute unit
 constexpr int kPgLeast = 4;      // blocks of a share at least, as far as there are that many
 
 struct PagedLayout {  // byte offsets into the workspace
