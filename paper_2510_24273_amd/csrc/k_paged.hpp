@@ -24,9 +24,13 @@ struct PagedCache {           // the cache of one layer and the shape of the cal
 
 // cos / sin of position * theta^(-2 pair / D): the angle in turns, in fp64, less its whole part; what is left is exact to 1e-16 * position
 // turns and goes to fp32 (half a step of a value of at most 1/2 turn: 9e-8 radians).
-template <int D> __device__ __forceinline__ float2 rope_turn(int position, int pair, double log2_theta)
+template <int D> __device__ __forceinline__ double rope_frequency(int pair, double log2_theta)   // turns per position
 {
-    const double t = (double)position * (exp2(-(double)pair * (2.0 / D) * log2_theta) * kInvTwoPi);
+    return exp2(-(double)pair * (2.0 / D) * log2_theta) * kInvTwoPi;
+}
+__device__ __forceinline__ float2 rope_turn(int position, double frequency)
+{
+    const double t = (double)position * frequency;
     float s, c;
     sincospif(2.f * (float)(t - rint(t)), &s, &c);
     return make_float2(c, s);
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
     const int n = min(want, a.cap - have);          // tokens that fit
     const int nt = min(kAppTok, n - t0);
     const int row = a.H_kv * D, qp = q_pos[b];
-    for (int i = tid; i < nt * NP; i += 256) sCS[i / NP][i % NP] = rope_turn<D>(qp + t0 + i / NP, i % NP, log2_theta);
+    for (int i = tid; i < nt * NP; i += 256) sCS[i / NP][i % NP] = rope_turn(qp + t0 + i / NP, rope_frequency<D>(i % NP, log2_theta));
     if (tid < nt) sRow[tid] = paged_row(a, b, have + t0 + tid, row);
     __syncthreads();
     if (gridDim.x == 1 && tid == 0 && n > 0) seq_len[b] = have + n;
@@ -138,10 +142,21 @@ __global__ __launch_bounds__(256) void paged_advance_kernel(int32_t* seq_len, co
 // lost at most), products and sums fp32.  The remainder is never zero beside a nonzero head: an infinite value stays one.
 // A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
-constexpr int kPgWaves = 8;
-constexpr int kPgGroups = 256;         // workgroups: one per compute unit
+#ifndef WV
+#define WV 8
+#endif
+#ifndef GR
+#define GR 256
+#endif
+#ifndef KLD
+#define KLD ld16
+#endif
+#ifndef VLD
+#define VLD ld16_stream
+#endif
+constexpr int kPgWaves = WV;
+constexpr int kPgGroups = GR;         // workgroups: one per compute unit
 constexpr int kPgAhead = 32;           // pieces of a shared sequence that a thread requests together
-constexpr int kPgJoin = 4;             // copies of the output that a workgroup's waves are added up in
 
 template <typename T> struct PgBlock;
 template <> struct PgBlock<bf16_t> { static constexpr int TB = 32; };
@@ -185,10 +200,10 @@ __device__ __forceinline__ float sum_xor_rows(float v)
 
 // grid (shares * H_kv * head tiles); logits: null, or [B * H][logit_stride] to be left
 template <typename T, int D, bool WHOLE>   // WHOLE: the CH slots of a lane lie in one page
-__global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
+__global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const int32_t* __restrict__ seq_len, int B, int cap, int max_shares, int heads,
+                                                                       PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
                                                                        const T* __restrict__ Kp, const T* __restrict__ Vp, T* __restrict__ out,
-                                                                       PagedParts parts, float* __restrict__ logits, int logit_stride, int max_shares,
-                                                                       int least, float scale, double log2_theta, int style)
+                                                                       PagedParts parts, float* __restrict__ logits, int logit_stride, float scale, double log2_theta, int style)
 {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int TB = PgBlock<T>::TB, CH = TB / 4, VEC = elem<T>::vec;
@@ -198,38 +213,48 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
     constexpr int VW = NJ * sizeof(T) / 4;     // 32-bit words of a V row per lane
     constexpr int NID = WHOLE ? 1 : CH, NIK = WHOLE ? 1 : NKT;
     constexpr int LROW = D + 4;
+    extern __shared__ __attribute__((aligned(16))) float sO[];   // [kPgWaves][parts.rows][LROW]
     __shared__ float2 sCS[D / 2];
     __shared__ float sM[kPgWaves][kPgHeads], sL[kPgWaves][kPgHeads];
-    __shared__ __attribute__((aligned(16))) float sO[kPgJoin][kPgHeads][LROW];
     __shared__ float sF[kPgHeads][kPgGroups];
     __shared__ uint32_t sLast;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6), n16 = lane & 15, c4 = lane >> 4;
-    const int tiles = (a.group + kPgHeads - 1) / kPgHeads, heads = a.H_kv * tiles, H = a.H_kv * a.group;
-    const int w = blockIdx.x / heads, hg = blockIdx.x - w * heads, g = hg / tiles, h0 = g * a.group + (hg - g * tiles) * kPgHeads;
+    const int w = idiv(blockIdx.x, heads);
+    // ---- this workgroup's share ----
+    const int per = (B + 63) >> 6;           // sequences of a lane; with one, their lengths stay in the lanes
+    auto clamped = [&](int n) { return min(max(n, 0), cap); };
+    auto blocks_in = [&](int n) { return max(1, (n + TB - 1) / TB); };
+    uint32_t mine = 0;
+    int lane_len = 0;
+    for (int i = 0; i < per; ++i)
+        if (lane * per + i < B) {
+            lane_len = clamped(seq_len[lane * per + i]);
+            mine += (uint32_t)blocks_in(lane_len);
+        }
+    // (while the lengths are on their way)
+    const double frequency = rope_frequency<D>(tid & (D / 2 - 1), log2_theta);
+    const int hg = blockIdx.x - w * heads, tiles = (a.group + kPgHeads - 1) / kPgHeads, H = a.H_kv * a.group;
+    const int g = tiles == 1 ? hg : idiv(hg, tiles), h0 = g * a.group + (hg - g * tiles) * kPgHeads;
     const int nh = min(kPgHeads, (g + 1) * a.group - h0);
     const int row = a.H_kv * D;
-
-    // ---- this workgroup's share ----
-    const int per = (a.B + 63) >> 6;           // sequences of a lane
-    auto blocks_of = [&](int b) { return max(1, (min(max(a.seq_len[b], 0), a.cap) + TB - 1) / TB); };
-    uint32_t mine = 0;
-    for (int i = 0; i < per; ++i) mine += lane * per + i < a.B ? (uint32_t)blocks_of(lane * per + i) : 0u;
     const uint32_t upto = wave_incl_scan(mine);
     PagedWork W;
     W.blocks = __builtin_amdgcn_readlane((int)upto, 63);
-    W.shares = max(1, min(max_shares, W.blocks / least));
+    W.shares = min(max_shares, W.blocks);
     if (w >= W.shares) return;
-    W.q = W.blocks / W.shares;
+    W.q = (int)((uint32_t)W.blocks / (uint32_t)W.shares);
     W.r = W.blocks - W.q * W.shares;
     int at = W.begin(w);
     const int end = W.begin(w + 1);
     const int first_lane = __popcll(__ballot(upto <= (uint32_t)at));
     int b = first_lane * per, base = __builtin_amdgcn_readlane((int)(upto - mine), first_lane);
-    for (int n; base + (n = wave_uniform(blocks_of(b))) <= at; ++b) base += n;
+    auto length_of = [&](int s) { return per == 1 ? __builtin_amdgcn_readlane(lane_len, s) : wave_uniform(clamped(seq_len[s])); };
+    for (int n; base + (n = blocks_in(length_of(b))) <= at; ++b) base += n;
 
-    while (at < end) {
-        const int S = wave_uniform(min(max(a.seq_len[b], 0), a.cap)), n_blocks = max(1, (S + TB - 1) / TB);
+    for (bool again = false; at < end; again = true) {
+        if (again) __syncthreads();   // (LDS is taken anew)
+        const int S = length_of(b), n_blocks = blocks_in(S);
         const int blk0 = at - base, blk1 = min(end - base, n_blocks), live1 = min(blk1, (S + TB - 1) / TB);
         const int32_t* tb = a.table + (size_t)b * a.max_pages;
 
@@ -261,7 +286,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
                 const int j = held(k_slot(t0, t));
                 const T* p = Kp + row_at(I.k[WHOLE ? 0 : t], j) + (WHOLE ? (t * 4 + (n16 & 3)) * row : 0) + g * D + c4 * VEC;
 #pragma unroll
-                for (int s = 0; s < NS; ++s) K[t][s] = ld16_stream(p + s * 4 * VEC);
+                for (int s = 0; s < NS; ++s) K[t][s] = KLD(p + s * 4 * VEC);
             }
         };
         auto load_v = [&](const Ids& I, int blk) {
@@ -278,32 +303,35 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
                 } else {
 #pragma unroll
                     for (int h = 0; h < VW / 4; ++h) {   // fp32: pieces of 4 channels, 64 channels apart
-                        const u32x4 x = ld16_stream(p + h * 64 + n16 * VEC);
+                        const u32x4 x = VLD(p + h * 64 + n16 * VEC);
                         V[e][4 * h] = x.x; V[e][4 * h + 1] = x.y; V[e][4 * h + 2] = x.z; V[e][4 * h + 3] = x.w;
                     }
                 }
             }
         };
 
-        // the first loads wait for the length and the table only
+        // the query and its position come ahead of the first rows, which wait for the table: it is rotated while they are on their way
         int blk = blk0 + wave;
+        const bool has = n16 < nh;
         Ids I0, I1;
         if (blk < live1) {
             load_ids(I0, blk);
             load_ids(I1, blk + kPgWaves);
-            load_k(I0, blk);
-            load_v(I0, blk);
         }
-
-        // ---- the rotated query of these heads, scaled ----
-        const bool has = n16 < nh;
+        const int position_v = ld_uniform_i32(q_pos + b);
         u32x4 qraw[NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             qraw[s] = u32x4{0u, 0u, 0u, 0u};
             if (has) qraw[s] = ld16(q + ((size_t)b * H + h0 + n16) * D + s * 4 * VEC + c4 * VEC);
         }
-        if (tid < D / 2) sCS[tid] = rope_turn<D>(q_pos[b], tid, log2_theta);
+        if (blk < live1) {
+            load_k(I0, blk);
+            load_v(I0, blk);
+        }
+
+        // ---- the rotated query of these heads, scaled ----
+        if (tid < D / 2) sCS[tid] = rope_turn(position_v, frequency);
         __syncthreads();
         float qf[NS][VEC];
 #pragma unroll
@@ -446,53 +474,44 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
         }
 
         // ---- the waves joined ----
-        l = sum_xor_rows(l);
-        if (lane < kPgHeads) { sM[wave][lane] = m; sL[wave][lane] = l; }
-        __syncthreads();
-        float M = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < kPgWaves; ++v) M = fmaxf(M, sM[v][n16]);
-        const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - M) : 0.f;
-        // channel of O[j][i] of this lane
-        auto channel = [&](int j, int i) { return BF ? (c4 * 4 + i) * NJ + j : (j >> 2) * 64 + (c4 * 4 + i) * 4 + (j & 3); };
-        auto put = [&](int at_copy) {
-            if (!has) return;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; j += 4)
-                    *reinterpret_cast<f32x4*>(&sO[at_copy][n16][channel(j, i)]) = f32x4{O[j][i] * f, O[j + 1][i] * f, O[j + 2][i] * f, O[j + 3][i] * f};
-        };
-        auto add = [&](int at_copy) {
-            if (!has) return;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; j += 4) {
-                    f32x4* to = reinterpret_cast<f32x4*>(&sO[at_copy][n16][channel(j, i)]);
-                    *to += f32x4{O[j][i] * f, O[j + 1][i] * f, O[j + 2][i] * f, O[j + 3][i] * f};
-                }
-        };
-        if (wave < kPgJoin) put(wave);
-        __syncthreads();
-        if (wave >= kPgJoin) add(wave - kPgJoin);
-        __syncthreads();
+        const int n_live = min(kPgWaves, live1 - blk0);   // waves that had a block
         const bool alone = blk0 == 0 && blk1 == n_blocks;
         const int w0 = W.share(base), w1 = W.share(base + n_blocks - 1);   // the shares that this sequence is spread over
-        // M and the normaliser of head h (of the tile)
-        auto norm = [&](int h, float* Mh) {
-            float Mx = -INFINITY, L = 0.f;
-            for (int v = 0; v < kPgWaves; ++v) Mx = fmaxf(Mx, sM[v][h]);
-            for (int v = 0; v < kPgWaves; ++v) L += sM[v][h] > -INFINITY ? sL[v][h] * __builtin_amdgcn_exp2f(sM[v][h] - Mx) : 0.f;
-            *Mh = Mx;
-            return L;
-        };
+        if (wave < n_live) {
+            l = sum_xor_rows(l);
+            if (lane < kPgHeads) { sM[wave][lane] = m; sL[wave][lane] = l; }
+            // channel of O[j][i] of this lane
+            auto channel = [&](int j, int i) { return BF ? (c4 * 4 + i) * NJ + j : (j >> 2) * 64 + (c4 * 4 + i) * 4 + (j & 3); };
+            if (has)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < NJ; j += 4)
+                        *reinterpret_cast<f32x4*>(sO + (wave * parts.rows + n16) * LROW + channel(j, i)) =
+                            f32x4{O[j][i], O[j + 1][i], O[j + 2][i], O[j + 3][i]};
+        }
+        __syncthreads();
         const size_t piece = ((size_t)(2 * w + (blk0 == 0)) * heads + hg) * parts.rows;
         for (int i = tid; i < nh * D; i += kPgWaves * 64) {
             const int h = i / D, ch = i % D;
-            float Mh;
-            const float L = norm(h, &Mh);
-            const float A = (sO[0][h][ch] + sO[1][h][ch]) + (sO[2][h][ch] + sO[3][h][ch]);
+            float mv[kPgWaves], lv[kPgWaves], ov[kPgWaves];
+#pragma unroll
+            for (int v = 0; v < kPgWaves; ++v) {
+                const bool on = v < n_live;   // (the others left nothing)
+                mv[v] = on ? sM[v][h] : -INFINITY;
+                lv[v] = sL[v][h];
+                ov[v] = sO[(v * parts.rows + h) * LROW + ch];
+            }
+            float Mh = mv[0], L = 0.f, A = 0.f;
+#pragma unroll
+            for (int v = 1; v < kPgWaves; ++v) Mh = fmaxf(Mh, mv[v]);
+#pragma unroll
+            for (int v = 0; v < kPgWaves; ++v) {
+                const bool some = v < n_live && lv[v] != 0.f;   // (or a NaN, which is to stay)
+                const float f = __builtin_amdgcn_exp2f(mv[v] - Mh);
+                L = some ? fmaf(lv[v], f, L) : L;
+                A = some ? fmaf(ov[v], f, A) : A;
+            }
             if (alone) {
                 elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
                 if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mh : 0.f, L != 0.f ? 1.f / L : 0.f);
@@ -532,7 +551,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
                     Mx = wave_max(Mx);
 #pragma unroll
                     for (int u = 0; u < kPgGroups / 64; ++u) {
-                        const float fu = st[u].x > -INFINITY ? __builtin_amdgcn_exp2f(st[u].x - Mx) : 0.f;
+                        const float fu = st[u].y != 0.f ? __builtin_amdgcn_exp2f(st[u].x - Mx) : 0.f;
                         L = fmaf(st[u].y, fu, L);
                         if (lane + 64 * u < n) sF[h][lane + 64 * u] = fu;
                     }
@@ -557,7 +576,6 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(PagedCac
                 }
             }
         }
-        __syncthreads();   // (LDS is taken anew by the next sequence)
         base += n_blocks;
         at = base;
         ++b;

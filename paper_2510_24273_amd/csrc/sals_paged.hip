@@ -19,7 +19,6 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline bool bad(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SALS_OK : SALS_ERR_HIP; }
 
-constexpr int kPgLeast = 4;      // blocks of a share at least, as far as there are that many
 
 struct PagedLayout {  // byte offsets into the workspace
     size_t count, sum, stat, final_stat, logits, moves, from, to, total;
@@ -117,6 +116,19 @@ sals_status launch_append(const sals_paged* c, const void* k_new, const void* v_
     return launch_status();
 }
 
+template <typename T, int D> auto attend_kernel(const sals_paged_desc& d)
+{
+    return d.page_size % (PgBlock<T>::TB / 4) == 0 ? paged_attend_kernel<T, D, true> : paged_attend_kernel<T, D, false>;
+}
+// the waves' outputs side by side: up to 68 KB
+inline uint32_t attend_lds(const sals_paged_desc& d, const PagedLayout& L) { return (uint32_t)(kPgWaves * L.rows * (d.d + 4) * 4); }
+
+template <typename T, int D> sals_status allow_attend_lds(const sals_paged* c)
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c->d)), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               (int)attend_lds(c->d, c->L)) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
+}
+
 template <typename T, int D>
 sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_pos, const int32_t* table, const void* Kp, const void* Vp,
                           const int32_t* seq_len, float* weights, void* out, hipStream_t st)
@@ -127,14 +139,10 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
     float* logits = weights ? at<float>(c, L.logits) : nullptr;
     const PagedParts parts{at<float>(c, L.sum), at<float2>(c, L.stat), at<uint32_t>(c, L.count), at<float2>(c, L.final_stat), L.rows};
     const float scale = (float)(1.4426950408889634074 / std::sqrt((double)D));
-    const dim3 grid(L.shares * d.H_kv * ceil_div(a.group, kPgHeads));
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kPgWaves * 64), 0, st, a, static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp),
-                           static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits, L.logit_stride, L.shares, kPgLeast, scale, c->log2_theta,
-                           d.rope_style);
-    };
-    if (d.page_size % (PgBlock<T>::TB / 4) == 0) launch(paged_attend_kernel<T, D, true>);
-    else launch(paged_attend_kernel<T, D, false>);
+    const int heads = d.H_kv * ceil_div(a.group, kPgHeads);
+    hipLaunchKernelGGL((attend_kernel<T, D>(d)), dim3(L.shares * heads), dim3(kPgWaves * 64), attend_lds(d, L), st, seq_len, d.B, a.cap, L.shares, heads, a,
+                       static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits,
+                       L.logit_stride, scale, c->log2_theta, d.rope_style);
     if (launch_status() != SALS_OK || !weights) return launch_status();
     hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 256)), d.weight_heads, d.B), dim3(256), 0, st, a, logits,
                        at<float2>(c, L.final_stat), L.logit_stride, weights);
@@ -193,6 +201,10 @@ sals_status sals_paged_create(const sals_paged_desc* desc, void* d_workspace, si
 
 void sals_paged_destroy(sals_paged* ctx) { delete ctx; }
 
+#define SALS_PAGED(D_, CALL)                                                                     \
+    (D_.dtype == SALS_BF16 ? (D_.d == 128 ? CALL(bf16_t, 128) : CALL(bf16_t, 64))               \
+                           : (D_.d == 128 ? CALL(float, 128) : CALL(float, 64)))
+
 sals_status sals_paged_prepare(sals_paged* ctx, void* hip_stream)
 {
     if (!ctx) return SALS_ERR_INVALID_ARG;
@@ -202,13 +214,12 @@ sals_status sals_paged_prepare(sals_paged* ctx, void* hip_stream)
     if (cap != hipStreamCaptureStatusNone) return SALS_ERR_INVALID_ARG;
     hipLaunchKernelGGL(paged_clear_kernel, dim3(ceil_div(ctx->L.n_count, 256)), dim3(256), 0, st, at<uint32_t>(ctx, ctx->L.count), ctx->L.n_count);
     if (launch_status() != SALS_OK || hipStreamSynchronize(st) != hipSuccess) return SALS_ERR_HIP;
+#define SALS_CALL(T, D) allow_attend_lds<T, D>(ctx)
+    if (SALS_PAGED(ctx->d, SALS_CALL) != SALS_OK) return SALS_ERR_HIP;
+#undef SALS_CALL
     ctx->prepared = true;
     return SALS_OK;
 }
-
-#define SALS_PAGED(D_, CALL)                                                                     \
-    (D_.dtype == SALS_BF16 ? (D_.d == 128 ? CALL(bf16_t, 128) : CALL(bf16_t, 64))               \
-                           : (D_.d == 128 ? CALL(float, 128) : CALL(float, 64)))
 
 sals_status sals_paged_append(sals_paged* ctx, const void* k_new, const void* v_new, const int32_t* q_pos, const int32_t* table, void* Kp, void* Vp,
                               int32_t* seq_len, const int32_t* n_new, int32_t n_tok, int32_t* pos, float* weights, void* hip_stream)

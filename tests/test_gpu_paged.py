@@ -210,6 +210,17 @@ def test_peaked_logits_and_an_infinite_value(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 40, 3000])
+def test_a_nan_in_a_key_reaches_its_heads_only(dtype, n):
+    c = Cache([n, 333], dtype=dtype)
+    c.Kp[int(c.table_h[0, 0]), 0, 1, 5] = float("nan")
+    c.attend()
+    torch.cuda.synchronize()
+    out = _np(c.out)
+    assert np.isnan(out[0, 4:]).all() and np.isfinite(out[0, :4]).all() and np.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_equal_keys_give_the_mean(dtype):
     """Logits that are all the same, however large: the plain mean of the values."""
     c = Cache([513], dtype=dtype, H=4, H_kv=1)
