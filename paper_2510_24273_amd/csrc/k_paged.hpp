@@ -142,21 +142,9 @@ __global__ __launch_bounds__(256) void paged_advance_kernel(int32_t* seq_len, co
 // lost at most), products and sums fp32.  The remainder is never zero beside a nonzero head: an infinite value stays one.
 // A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
-#ifndef WV
-#define WV 8
-#endif
-#ifndef GR
-#define GR 256
-#endif
-#ifndef KLD
-#define KLD ld16
-#endif
-#ifndef VLD
-#define VLD ld16_stream
-#endif
-constexpr int kPgWaves = WV;
-constexpr int kPgGroups = GR;         // workgroups: one per compute unit
-constexpr int kPgAhead = 32;           // pieces of a shared sequence that a thread requests together
+constexpr int kPgWaves = 8;
+constexpr int kPgGroups = 256;         // workgroups: one per compute unit
+constexpr int kPgAhead = 8;            // pieces of a shared sequence that a thread requests together
 
 template <typename T> struct PgBlock;
 template <> struct PgBlock<bf16_t> { static constexpr int TB = 32; };
@@ -175,7 +163,7 @@ struct PagedWork {
 struct PagedParts {               // pieces of shared sequences: slot 2 w of share w for one that began before it, 2 w + 1 for one that goes on behind
     float* sum;                   // [2 shares][heads of the grid][rows][D]
     float2* stat;                 // [2 shares][heads of the grid][rows]
-    uint32_t* count;              // [B][heads of the grid]
+    uint32_t* count;              // [B][heads of the grid], zero between launches
     float2* final_stat;           // [B * H]: maximum, 1 / sum
     int rows;                     // query heads of a workgroup at most
 };
@@ -183,8 +171,27 @@ struct PagedParts {               // pieces of shared sequences: slot 2 w of sha
 // Stores and loads that pass the caches of the compute unit and of its die, for what one workgroup leaves to another of the same
 // launch: ordinary ones would need a write-back and an invalidation of a whole L2 around them.  A workgroup's stores
 // are done, for every workgroup of the device, behind device_stores_done() in every thread and a barrier.
-__device__ __forceinline__ void st_device(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float ld_device(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ f32x4 ld4_device(const float* p)
+{
+    const uint64_t* u = reinterpret_cast<const uint64_t*>(p);
+    const uint64_t a = __hip_atomic_load(u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), b = __hip_atomic_load(u + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return f32x4{__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)), __uint_as_float((uint32_t)b), __uint_as_float((uint32_t)(b >> 32))};
+}
+__device__ __forceinline__ void st4_device(float* p, const f32x4& v)
+{
+    uint64_t* u = reinterpret_cast<uint64_t*>(p);
+    __hip_atomic_store(u, (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(u + 1, (uint64_t)__float_as_uint(v.w) << 32 | __float_as_uint(v.z), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 ld2_device(const float2* p)
+{
+    const uint64_t a = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
+}
+__device__ __forceinline__ void st2_device(float2* p, float2 v)
+{
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ void device_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float max_xor_rows(float v)   // over the four lanes that hold a head
@@ -200,7 +207,7 @@ __device__ __forceinline__ float sum_xor_rows(float v)
 
 // grid (shares * H_kv * head tiles); logits: null, or [B * H][logit_stride] to be left
 template <typename T, int D, bool WHOLE>   // WHOLE: the CH slots of a lane lie in one page
-__global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const int32_t* __restrict__ seq_len, int B, int cap, int max_shares, int heads,
+__global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const int32_t* __restrict__ seq_len, int B, int cap, int kv_heads, int tiles,
                                                                        PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
                                                                        const T* __restrict__ Kp, const T* __restrict__ Vp, T* __restrict__ out,
                                                                        PagedParts parts, float* __restrict__ logits, int logit_stride, float scale, double log2_theta, int style)
@@ -213,38 +220,49 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     constexpr int VW = NJ * sizeof(T) / 4;     // 32-bit words of a V row per lane
     constexpr int NID = WHOLE ? 1 : CH, NIK = WHOLE ? 1 : NKT;
     constexpr int LROW = D + 4;
-    extern __shared__ __attribute__((aligned(16))) float sO[];   // [kPgWaves][parts.rows][LROW]
-    __shared__ float2 sCS[D / 2];
+    constexpr int THREADS = kPgWaves * 64;
+    extern __shared__ __attribute__((aligned(16))) float sO[];   // [kPgWaves][parts.rows][LROW], then the factors of pieces
+    __shared__ u32x4 sQ[2][BF ? 3 : 1][NS][64];   // the query as the matrix instructions take it
     __shared__ float sM[kPgWaves][kPgHeads], sL[kPgWaves][kPgHeads];
-    __shared__ float sF[kPgHeads][kPgGroups];
+    __shared__ __attribute__((aligned(16))) f32x4 sX[THREADS];
     __shared__ uint32_t sLast;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6), n16 = lane & 15, c4 = lane >> 4;
-    const int w = idiv(blockIdx.x, heads);
+    const int tid0 = threadIdx.x, wave = wave_uniform(tid0 >> 6);
     // ---- this workgroup's share ----
     const int per = (B + 63) >> 6;           // sequences of a lane; with one, their lengths stay in the lanes
     auto clamped = [&](int n) { return min(max(n, 0), cap); };
     auto blocks_in = [&](int n) { return max(1, (n + TB - 1) / TB); };
     uint32_t mine = 0;
     int lane_len = 0;
+    const int lane0 = tid0 & 63;
     for (int i = 0; i < per; ++i)
-        if (lane * per + i < B) {
-            lane_len = clamped(seq_len[lane * per + i]);
+        if (lane0 * per + i < B) {
+            lane_len = clamped(seq_len[lane0 * per + i]);
             mine += (uint32_t)blocks_in(lane_len);
         }
     // (while the lengths are on their way)
-    const double frequency = rope_frequency<D>(tid & (D / 2 - 1), log2_theta);
-    const int hg = blockIdx.x - w * heads, tiles = (a.group + kPgHeads - 1) / kPgHeads, H = a.H_kv * a.group;
-    const int g = tiles == 1 ? hg : idiv(hg, tiles), h0 = g * a.group + (hg - g * tiles) * kPgHeads;
-    const int nh = min(kPgHeads, (g + 1) * a.group - h0);
+    const double frequency = rope_frequency<D>(tid0 & (D / 2 - 1), log2_theta);
     const int row = a.H_kv * D;
     const uint32_t upto = wave_incl_scan(mine);
     PagedWork W;
     W.blocks = __builtin_amdgcn_readlane((int)upto, 63);
-    W.shares = min(max_shares, W.blocks);
+    // Two neighbouring KV heads of a workgroup, four waves for each, read twice as long pieces of memory, and the channels that are slow
+    // for every fourth 256 bytes are shared out; a sequence then has twice as many pieces to join.  From 16 blocks for each workgroup
+    // on that is worth it (32 heads, 16 x 4096 slots: 177 -> 167 us; 8 heads, 8 x 8191: 62 -> 60; 8 heads, 4100 slots: 13.7 -> 18.7).
+    const int single = kv_heads * tiles;
+    const bool two = tiles == 1 && !(kv_heads & 1) && W.blocks >= idiv(16 * kPgGroups, single);
+    const int HPW = two ? 2 : 1, WPH = two ? kPgWaves / 2 : kPgWaves, heads = two ? single >> 1 : single;
+    W.shares = min(max(1, idiv(kPgGroups, heads)), W.blocks);
+    const int w = idiv(blockIdx.x, heads);
     if (w >= W.shares) return;
     W.q = (int)((uint32_t)W.blocks / (uint32_t)W.shares);
     W.r = W.blocks - W.q * W.shares;
+    // a workgroup's query heads are consecutive, nh for each of its KV heads
+    const int hg = blockIdx.x - w * heads, sub = two ? wave >> 2 : 0, H = a.H_kv * a.group;
+    const int g = two ? 2 * hg + sub : tiles == 1 ? hg : idiv(hg, tiles);
+    const int first_head = tiles == 1 ? hg * HPW * a.group : g * a.group + (hg - g * tiles) * kPgHeads;
+    const int nh = min(kPgHeads, (g + 1) * a.group - first_head - sub * a.group), h0 = first_head + sub * a.group;
+    const int wave_of = two ? wave & 3 : wave;   // of the KV head
     int at = W.begin(w);
     const int end = W.begin(w + 1);
     const int first_lane = __popcll(__ballot(upto <= (uint32_t)at));
@@ -254,6 +272,10 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
 
     for (bool again = false; at < end; again = true) {
         if (again) __syncthreads();   // (LDS is taken anew)
+        // (new values for the compiler: what follows from them is computed where it is wanted, not kept through the stream)
+        int tid = tid0;
+        asm volatile("" : "+v"(tid));
+        int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
         const int S = length_of(b), n_blocks = blocks_in(S);
         const int blk0 = at - base, blk1 = min(end - base, n_blocks), live1 = min(blk1, (S + TB - 1) / TB);
         const int32_t* tb = a.table + (size_t)b * a.max_pages;
@@ -286,7 +308,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                 const int j = held(k_slot(t0, t));
                 const T* p = Kp + row_at(I.k[WHOLE ? 0 : t], j) + (WHOLE ? (t * 4 + (n16 & 3)) * row : 0) + g * D + c4 * VEC;
 #pragma unroll
-                for (int s = 0; s < NS; ++s) K[t][s] = KLD(p + s * 4 * VEC);
+                for (int s = 0; s < NS; ++s) K[t][s] = ld16(p + s * 4 * VEC);
             }
         };
         auto load_v = [&](const Ids& I, int blk) {
@@ -303,7 +325,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                 } else {
 #pragma unroll
                     for (int h = 0; h < VW / 4; ++h) {   // fp32: pieces of 4 channels, 64 channels apart
-                        const u32x4 x = VLD(p + h * 64 + n16 * VEC);
+                        const u32x4 x = ld16_stream(p + h * 64 + n16 * VEC);
                         V[e][4 * h] = x.x; V[e][4 * h + 1] = x.y; V[e][4 * h + 2] = x.z; V[e][4 * h + 3] = x.w;
                     }
                 }
@@ -311,19 +333,26 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         };
 
         // the query and its position come ahead of the first rows, which wait for the table: it is rotated while they are on their way
-        int blk = blk0 + wave;
-        const bool has = n16 < nh;
+        int blk = blk0 + wave_of;
         Ids I0, I1;
         if (blk < live1) {
             load_ids(I0, blk);
-            load_ids(I1, blk + kPgWaves);
+            load_ids(I1, blk + WPH);
         }
+        // a thread's pair of channels in some of the 16 columns of every KV head (columns without a query head are zero)
+        constexpr int COLS = THREADS / (D / 2), NQ = 2 * kPgHeads / COLS;
+        const int pair = tid % (D / 2), ch1 = style ? 2 * pair : pair, ch2 = style ? 2 * pair + 1 : pair + D / 2;
         const int position_v = ld_uniform_i32(q_pos + b);
-        u32x4 qraw[NS];
+        T q1[NQ], q2[NQ];
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            qraw[s] = u32x4{0u, 0u, 0u, 0u};
-            if (has) qraw[s] = ld16(q + ((size_t)b * H + h0 + n16) * D + s * 4 * VEC + c4 * VEC);
+        for (int k = 0; k < NQ; ++k) {
+            const int col = tid / (D / 2) + k * COLS, h = col % kPgHeads;
+            q1[k] = q2[k] = T(0);
+            if (h < nh && col < HPW * kPgHeads) {
+                const T* p = q + ((size_t)b * H + first_head + col / kPgHeads * nh + h) * D;
+                q1[k] = p[ch1];
+                q2[k] = p[ch2];
+            }
         }
         if (blk < live1) {
             load_k(I0, blk);
@@ -331,71 +360,56 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         }
 
         // ---- the rotated query of these heads, scaled ----
-        if (tid < D / 2) sCS[tid] = rope_turn(position_v, frequency);
-        __syncthreads();
-        float qf[NS][VEC];
+        {
+            const float2 cs = rope_turn(position_v, frequency);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) elem<T>::unpack(qraw[s], qf[s]);
-        if (style) {
+            for (int k = 0; k < NQ; ++k) {
+                const int col = tid / (D / 2) + k * COLS;
+                if (col >= HPW * kPgHeads) break;
+                const float x = elem<T>::load(&q1[k]), y = elem<T>::load(&q2[k]);
+                float r[2] = {fmaf(x, cs.x, -(y * cs.y)) * scale, fmaf(y, cs.x, x * cs.y) * scale};
+                const int ch[2] = {ch1, ch2};
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < VEC; e += 2) {
-                    const float2 cs = sCS[(s * 4 * VEC + c4 * VEC + e) / 2];
-                    const float x = qf[s][e], y = qf[s][e + 1];
-                    qf[s][e] = fmaf(x, cs.x, -(y * cs.y)) * scale;
-                    qf[s][e + 1] = fmaf(y, cs.x, x * cs.y) * scale;
-                }
-        } else {
-#pragma unroll
-            for (int s = 0; s < NS / 2; ++s)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float2 cs = sCS[s * 4 * VEC + c4 * VEC + e];
-                    const float x = qf[s][e], y = qf[s + NS / 2][e];
-                    qf[s][e] = fmaf(x, cs.x, -(y * cs.y)) * scale;
-                    qf[s + NS / 2][e] = fmaf(y, cs.x, x * cs.y) * scale;
-                }
-        }
-        u32x4 qp[BF ? 3 : 1][NS];
-        if constexpr (BF) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int k = 0; k < 3; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t lo = f32_to_bf16(qf[s][2 * e]), hi = f32_to_bf16(qf[s][2 * e + 1]);
-                        qf[s][2 * e] -= bf16_to_f32((bf16_t)lo);
-                        qf[s][2 * e + 1] -= bf16_to_f32((bf16_t)hi);
-                        qp[k][s][e] = lo | hi << 16;
+                    for (int k3 = 0; k3 < (BF ? 3 : 1); ++k3) {
+                        T* to = reinterpret_cast<T*>(&sQ[col / kPgHeads][k3][ch[u] / (4 * VEC)][ch[u] / VEC % 4 * 16 + col % kPgHeads]) + ch[u] % VEC;
+                        elem<T>::store(to, r[u]);
+                        if constexpr (BF) r[u] -= (float)(__bf16)r[u];
                     }
+            }
         }
+        __syncthreads();
 
         // ---- the stream ----
         float m = -INFINITY, l = 0.f;
         f32x4 O[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (; blk < live1; blk += kPgWaves) {
+        for (; blk < live1; blk += WPH) {
             const int t0 = blk * TB;
-            const bool more = blk + kPgWaves < live1;
+            const bool more = blk + WPH < live1;
             f32x4 x[NKT];
 #pragma unroll
-            for (int t = 0; t < NKT; ++t) {
-                x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < NKT; ++t) x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            int at_lane = lane;
+            asm volatile("" : "+v"(at_lane));   // (read from LDS for every block: the registers are wanted for rows)
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    if constexpr (BF) {
+            for (int s = 0; s < NS; ++s)
 #pragma unroll
-                        for (int k = 2; k >= 0; --k)
-                            x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, K[t][s]), __builtin_bit_cast(bf16x8, qp[k][s]), x[t], 0, 0, 0);
-                    } else {
+                for (int k = (BF ? 2 : 0); k >= 0; --k) {
+                    const u32x4 qv = sQ[sub][k][s][at_lane];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(K[t][s][e]), qf[s][e], x[t], 0, 0, 0);
+                    for (int t = 0; t < NKT; ++t) {
+                        if constexpr (BF) {
+                            x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, K[t][s]), __builtin_bit_cast(bf16x8, qv), x[t], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(K[t][s][e]), __uint_as_float(qv[e]), x[t], 0, 0, 0);
+                        }
                     }
                 }
-            }
             // which of this lane's slots count (slot t0 + CH c4 + e is x[e / 4][e % 4])
             bool whole = t0 + TB <= S;
 #pragma unroll
@@ -409,11 +423,12 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             }
             const uint64_t part_of = __ballot(!whole);
             Ids I2;
+            __builtin_amdgcn_sched_barrier(0);
             if (more) {
-                load_ids(I2, blk + 2 * kPgWaves);
-                load_k(I1, blk + kPgWaves);
+                load_ids(I2, blk + 2 * WPH);
+                load_k(I1, blk + WPH);
             }
-            if (logits && has) {
+            if (logits && n16 < nh) {
                 float* to = logits + (size_t)((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
 #pragma unroll
                 for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = x[t];
@@ -468,21 +483,24 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(V[e][j]), p[e], O[j], 0, 0, 0);
             }
-            if (more) load_v(I1, blk + kPgWaves);
+            __builtin_amdgcn_sched_barrier(0);   // (the rows behind take these registers, not others)
+            if (more) load_v(I1, blk + WPH);
             I0 = I1;
             I1 = I2;
         }
 
         // ---- the waves joined ----
-        const int n_live = min(kPgWaves, live1 - blk0);   // waves that had a block
+        asm volatile("" : "+v"(tid));
+        lane = tid & 63; n16 = lane & 15; c4 = lane >> 4;
+        const int n_live = min(WPH, live1 - blk0);        // waves of a KV head that had a block
         const bool alone = blk0 == 0 && blk1 == n_blocks;
         const int w0 = W.share(base), w1 = W.share(base + n_blocks - 1);   // the shares that this sequence is spread over
-        if (wave < n_live) {
+        if (wave_of < n_live) {
             l = sum_xor_rows(l);
             if (lane < kPgHeads) { sM[wave][lane] = m; sL[wave][lane] = l; }
             // channel of O[j][i] of this lane
             auto channel = [&](int j, int i) { return BF ? (c4 * 4 + i) * NJ + j : (j >> 2) * 64 + (c4 * 4 + i) * 4 + (j & 3); };
-            if (has)
+            if (n16 < nh)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -491,33 +509,45 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                             f32x4{O[j][i], O[j + 1][i], O[j + 2][i], O[j + 3][i]};
         }
         __syncthreads();
-        const size_t piece = ((size_t)(2 * w + (blk0 == 0)) * heads + hg) * parts.rows;
-        for (int i = tid; i < nh * D; i += kPgWaves * 64) {
-            const int h = i / D, ch = i % D;
-            float mv[kPgWaves], lv[kPgWaves], ov[kPgWaves];
+        // four channels of a head at a time: quad -> (KV head, query head, channels)
+        const int quads = HPW * nh * (D / 4);
+        auto finish = [&](int quad, f32x4 A, float Mh, float L) {
+            const size_t h = (size_t)b * H + first_head + quad / (D / 4);
+            const float inv = L != 0.f ? 1.f / L : 0.f;   // (nothing attended: zero)
+            const f32x4 y = A * inv;
+            T* to = out + h * D + quad % (D / 4) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) elem<T>::store(to + e, y[e]);
+            if (quad % (D / 4) == 0) parts.final_stat[h] = make_float2(L != 0.f ? Mh : 0.f, inv);
+        };
+        const size_t piece = ((size_t)(2 * w + (blk0 == 0)) * heads + hg) * (HPW * parts.rows);
+        for (int quad = tid; quad < quads; quad += THREADS) {
+            const int hh = quad / (D / 4), s = two && hh >= nh ? 1 : 0, h = hh - s * nh;
+            float mv[kPgWaves], lv[kPgWaves];
+            f32x4 ov[kPgWaves];
 #pragma unroll
             for (int v = 0; v < kPgWaves; ++v) {
-                const bool on = v < n_live;   // (the others left nothing)
-                mv[v] = on ? sM[v][h] : -INFINITY;
-                lv[v] = sL[v][h];
-                ov[v] = sO[(v * parts.rows + h) * LROW + ch];
+                const int wv = min(s * WPH + v, kPgWaves - 1);
+                mv[v] = v < n_live ? sM[wv][h] : -INFINITY;   // (the others left nothing)
+                lv[v] = sL[wv][h];
+                ov[v] = *reinterpret_cast<const f32x4*>(sO + (wv * parts.rows + h) * LROW + quad % (D / 4) * 4);
             }
-            float Mh = mv[0], L = 0.f, A = 0.f;
+            float Mh = mv[0], L = 0.f;
+            f32x4 A = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int v = 1; v < kPgWaves; ++v) Mh = fmaxf(Mh, mv[v]);
 #pragma unroll
-            for (int v = 0; v < kPgWaves; ++v) {
-                const bool some = v < n_live && lv[v] != 0.f;   // (or a NaN, which is to stay)
-                const float f = __builtin_amdgcn_exp2f(mv[v] - Mh);
-                L = some ? fmaf(lv[v], f, L) : L;
-                A = some ? fmaf(ov[v], f, A) : A;
-            }
+            for (int v = 0; v < kPgWaves; ++v)
+                if (v < n_live && lv[v] != 0.f) {   // (or a NaN, which is to stay)
+                    const float f = __builtin_amdgcn_exp2f(mv[v] - Mh);
+                    L = fmaf(lv[v], f, L);
+                    A += ov[v] * f;
+                }
             if (alone) {
-                elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
-                if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? Mh : 0.f, L != 0.f ? 1.f / L : 0.f);
+                finish(quad, A, Mh, L);
             } else {
-                st_device(parts.sum + (piece + h) * D + ch, A);
-                if (ch == 0) { st_device(&parts.stat[piece + h].x, Mh); st_device(&parts.stat[piece + h].y, L); }
+                st4_device(parts.sum + (piece + hh) * D + quad % (D / 4) * 4, A);
+                if (quad % (D / 4) == 0) st2_device(parts.stat + piece + hh, make_float2(Mh, L));
             }
         }
         if (!alone) {
@@ -527,52 +557,67 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             if (tid == 0) sLast = arrive(parts.count + (size_t)b * heads + hg, (uint32_t)(w1 - w0 + 1)) == (uint32_t)(w1 - w0);
             __syncthreads();
             if (sLast) {
+                asm volatile("" : "+v"(tid));
+                lane = tid & 63;
                 // (share, kind) of the pieces: the first share's goes on behind it, the others' began before
-                auto piece_of = [&](int v) { return ((size_t)(2 * v + (v == w0)) * heads + hg) * parts.rows; };
+                auto piece_of = [&](int v) { return ((size_t)(2 * v + (v == w0)) * heads + hg) * (HPW * parts.rows); };
                 const int n = w1 - w0 + 1;
-                auto sums = [&](float (&x)[kPgAhead], int i, int v) {   // of column i = (head, channel), shares w0 + v ...
+                // the statistics of a head are a wave's: the first of them, then this thread's first sums, then what follows from the former
+                auto stat_of = [&](int hh, int v) { return v < n ? ld2_device(parts.stat + piece_of(w0 + v) + hh) : make_float2(-INFINITY, 0.f); };
+                float2 st = make_float2(-INFINITY, 0.f);
+                if (wave < HPW * nh) st = stat_of(wave, lane);
+                // with fewer quads than threads several threads share a quad's pieces
+                const int sharers = quads < THREADS ? idiv(THREADS, quads) : 1, mine_of = sharers > 1 ? idiv(tid, quads) : 0;
+                f32x4 x[kPgAhead];
+                auto request = [&](int quad, int v) {
 #pragma unroll
-                    for (int u = 0; u < kPgAhead; ++u) x[u] = ld_device(parts.sum + piece_of(w0 + min(v + u, n - 1)) * D + i);
-                };
-                float x[kPgAhead];
-                sums(x, min(tid, nh * D - 1), 0);
-                for (int h = wave; h < nh; h += kPgWaves) {   // a wave takes a head's statistics
-                    float2 st[kPgGroups / 64];
-                    float Mx = -INFINITY, L = 0.f;
-#pragma unroll
-                    for (int u = 0; u < kPgGroups / 64; ++u) {
-                        st[u] = make_float2(-INFINITY, 0.f);
-                        if (lane + 64 * u < n) {
-                            const float2* p = parts.stat + piece_of(w0 + lane + 64 * u) + h;
-                            st[u] = make_float2(ld_device(&p->x), ld_device(&p->y));
-                        }
-                        Mx = fmaxf(Mx, st[u].x);
+                    for (int u = 0; u < kPgAhead; ++u) {
+                        x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        if (v + u * sharers < n) x[u] = ld4_device(parts.sum + piece_of(w0 + v + u * sharers) * D + quad * 4);
                     }
-                    Mx = wave_max(Mx);
-#pragma unroll
-                    for (int u = 0; u < kPgGroups / 64; ++u) {
-                        const float fu = st[u].y != 0.f ? __builtin_amdgcn_exp2f(st[u].x - Mx) : 0.f;
-                        L = fmaf(st[u].y, fu, L);
-                        if (lane + 64 * u < n) sF[h][lane + 64 * u] = fu;
+                };
+                int quad = sharers > 1 ? tid - mine_of * quads : tid;
+                const bool works = mine_of < sharers && quad < quads;
+                if (works) request(quad, mine_of);
+                for (int hh = wave; hh < HPW * nh; hh += kPgWaves) {
+                    if (hh != wave) st = stat_of(hh, lane);
+                    float Mx = wave_max(st.x);
+                    for (int v = kWave; v < n; v += kWave) Mx = fmaxf(Mx, wave_max(stat_of(hh, v + lane).x));
+                    float L = 0.f;
+                    for (int v = 0; v < n; v += kWave) {
+                        if (v > 0) st = stat_of(hh, v + lane);
+                        const float f = st.y != 0.f ? __builtin_amdgcn_exp2f(st.x - Mx) : 0.f;   // (NaN stays NaN)
+                        L = fmaf(st.y, f, L);
+                        if (v + lane < n) sO[hh * n + v + lane] = f;
                     }
                     L = wave_sum(L);
-                    if (lane == 0) { sM[0][h] = Mx; sL[0][h] = L; }
+                    if (lane == 0) { sM[hh / kPgHeads][hh % kPgHeads] = Mx; sL[hh / kPgHeads][hh % kPgHeads] = L; }
                 }
                 __syncthreads();
-                for (int i = tid; i < nh * D; i += kPgWaves * 64) {
-                    const int h = i / D, ch = i % D;
-                    float A = 0.f;
-                    for (int v = 0; v < n; v += kPgAhead) {
-                        if (v > 0 || i != tid) sums(x, i, v);
+                for (int q0 = 0; q0 < quads; q0 += THREADS, quad += THREADS) {
+                    f32x4 A = {0.f, 0.f, 0.f, 0.f};
+                    const int hh = quad / (D / 4);
+                    if (works && quad < quads) {
+                        for (int v = mine_of; v < n; v += kPgAhead * sharers) {
+                            if (q0 > 0 || v > mine_of) request(quad, v);
+                            float f[kPgAhead];
 #pragma unroll
-                        for (int u = 0; u < kPgAhead; ++u) {
-                            const float fu = v + u < n ? sF[h][min(v + u, n - 1)] : 0.f;
-                            A = fu != 0.f ? fmaf(x[u], fu, A) : A;
+                            for (int u = 0; u < kPgAhead; ++u) f[u] = sO[hh * n + min(v + u * sharers, n - 1)];
+#pragma unroll
+                            for (int u = 0; u < kPgAhead; ++u)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) A[e] = fmaf(f[u] != 0.f ? x[u][e] : 0.f, f[u], A[e]);   // (x is zero behind the last piece)
+                        }
+                        if (sharers == 1) finish(quad, A, sM[hh / kPgHeads][hh % kPgHeads], sL[hh / kPgHeads][hh % kPgHeads]);
+                    }
+                    if (sharers > 1) {
+                        sX[tid] = A;
+                        __syncthreads();
+                        if (tid < quads) {
+                            for (int k = 1; k < sharers; ++k) A += sX[tid + k * quads];
+                            finish(tid, A, sM[hh / kPgHeads][hh % kPgHeads], sL[hh / kPgHeads][hh % kPgHeads]);
                         }
                     }
-                    const float L = sL[0][h];
-                    elem<T>::store(out + ((size_t)b * H + h0 + h) * D + ch, L != 0.f ? A / L : 0.f);
-                    if (ch == 0) parts.final_stat[(size_t)b * H + h0 + h] = make_float2(L != 0.f ? sM[0][h] : 0.f, L != 0.f ? 1.f / L : 0.f);
                 }
             }
         }

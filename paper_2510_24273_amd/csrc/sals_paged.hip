@@ -22,7 +22,7 @@ inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SA
 
 struct PagedLayout {  // byte offsets into the workspace
     size_t count, sum, stat, final_stat, logits, moves, from, to, total;
-    int n_count, shares, rows, move_cap, logit_stride;
+    int n_count, tiles, groups, rows, lds, move_cap, logit_stride;   // of the attention: head tiles, workgroups, query heads of one, LDS
 };
 
 inline int capacity(const sals_paged_desc& d) { return d.max_pages * d.page_size; }
@@ -50,17 +50,20 @@ PagedLayout make_layout(const sals_paged_desc& d)
 {
     PagedLayout L{};
     const size_t H = (size_t)d.B * d.H_q, cap = (size_t)capacity(d);
-    const int group = d.H_q / d.H_kv, heads = d.H_kv * ceil_div(group, kPgHeads), tb = d.dtype == SALS_BF16 ? PgBlock<bf16_t>::TB : PgBlock<float>::TB;
-    L.n_count = d.B * heads;
-    // a workgroup per compute unit, no more than there can be blocks
-    L.shares = (int)std::max<int64_t>(1, std::min<int64_t>(kPgGroups / heads, (int64_t)d.B * ceil_div((int)cap, tb)));
+    const int group = d.H_q / d.H_kv, tiles = ceil_div(group, kPgHeads), single = d.H_kv * tiles, pairs = tiles == 1 && d.H_kv % 2 == 0 ? single / 2 : single;
+    L.tiles = tiles;
+    L.n_count = d.B * single;
+    // the kernel takes one KV head for each workgroup or two, by the lengths: room for either
+    const int one = std::max(1, kPgGroups / single), two = std::max(1, kPgGroups / pairs);   // shares
+    L.groups = std::max(one * single, two * pairs);
     L.rows = std::min(group, kPgHeads);
+    L.lds = 4 * std::max(kPgWaves * L.rows * (d.d + 4), L.rows * std::max(one, 2 * two));   // the waves' sums, or the factors of the pieces: up to 68 KB
     L.logit_stride = ceil_div((int)cap, 32) * 32;
     L.move_cap = (int)cap / 2 + 1;   // (no more than half of the slots can move below the others)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes); return r; };
     L.count = take((size_t)L.n_count * 4);
-    const size_t pieces = (size_t)2 * L.shares * heads * L.rows;
+    const size_t pieces = (size_t)2 * L.rows * std::max(one * single, 2 * two * pairs);
     L.sum = take(pieces * d.d * 4);
     L.stat = take(pieces * 8);
     L.final_stat = take(H * 8);
@@ -116,17 +119,14 @@ sals_status launch_append(const sals_paged* c, const void* k_new, const void* v_
     return launch_status();
 }
 
-template <typename T, int D> auto attend_kernel(const sals_paged_desc& d)
+template <typename T, int D> auto attend_kernel(const sals_paged* c)
 {
-    return d.page_size % (PgBlock<T>::TB / 4) == 0 ? paged_attend_kernel<T, D, true> : paged_attend_kernel<T, D, false>;
+    return c->d.page_size % (PgBlock<T>::TB / 4) == 0 ? paged_attend_kernel<T, D, true> : paged_attend_kernel<T, D, false>;
 }
-// the waves' outputs side by side: up to 68 KB
-inline uint32_t attend_lds(const sals_paged_desc& d, const PagedLayout& L) { return (uint32_t)(kPgWaves * L.rows * (d.d + 4) * 4); }
-
 template <typename T, int D> sals_status allow_attend_lds(const sals_paged* c)
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c->d)), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               (int)attend_lds(c->d, c->L)) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c)), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               c->L.lds) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
 }
 
 template <typename T, int D>
@@ -139,8 +139,7 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
     float* logits = weights ? at<float>(c, L.logits) : nullptr;
     const PagedParts parts{at<float>(c, L.sum), at<float2>(c, L.stat), at<uint32_t>(c, L.count), at<float2>(c, L.final_stat), L.rows};
     const float scale = (float)(1.4426950408889634074 / std::sqrt((double)D));
-    const int heads = d.H_kv * ceil_div(a.group, kPgHeads);
-    hipLaunchKernelGGL((attend_kernel<T, D>(d)), dim3(L.shares * heads), dim3(kPgWaves * 64), attend_lds(d, L), st, seq_len, d.B, a.cap, L.shares, heads, a,
+    hipLaunchKernelGGL((attend_kernel<T, D>(c)), dim3(L.groups), dim3(kPgWaves * 64), L.lds, st, seq_len, d.B, a.cap, d.H_kv, L.tiles, a,
                        static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits,
                        L.logit_stride, scale, c->log2_theta, d.rope_style);
     if (launch_status() != SALS_OK || !weights) return launch_status();

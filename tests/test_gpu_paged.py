@@ -233,6 +233,22 @@ def test_equal_keys_give_the_mean(dtype):
     assert (np.abs(_np(c.out) - 3.0) <= 3.0 * (HALF[dtype] + 2.0 ** -13)).all()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("H,H_kv,P,lens", [(32, 32, 16, [1500, 2600, 0, 3333, 1]), (24, 8, 24, [9000, 7, 8500, 0, 300]), (20, 2, 64, [66000, 300]), (6, 6, 7, [12001, 12000]),
+                                           (7, 7, 16, [9000, 9000])])
+def test_long_batches(H, H_kv, P, lens, dtype, d):
+    """Work for two KV heads in a workgroup (and an odd number of them)."""
+    c = Cache(lens, H=H, H_kv=H_kv, P=P, d=d, dtype=dtype, lists=1, holes=[(0, 5, -1)])
+    before = c.weights.clone()
+    c.attend()
+    torch.cuda.synchronize()
+    c.check_attend(before)
+    first = c.out.clone()
+    c.attend(weights=False)
+    torch.cuda.synchronize()
+    assert torch.equal(first, c.out)
+
+
 def test_many_ragged_sequences():
     rng = np.random.default_rng(3)
     lens = [int(x) for x in np.exp(rng.uniform(0, np.log(2500), 70))]
