@@ -645,142 +645,389 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
 }
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------
+// A list's n_keep slots of the largest keys, and the moves that bring them below slot n_keep.  One workgroup per list; a wave holds
+// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps; longer lists are read anew in every pass.
+//
+// Threshold: the key and the slot of the last one that stays.  Where up to kEvFew leave they are found one by one (the lowest first).
+// Otherwise a histogram over the keys' leading 12 bits (keys are the floats' bits in order, so eight bins for a factor of two) names the
+// bin, as a rule of a few dozen, whose members are ranked against each other in LDS; larger ones are split by the next 12 and 8 bits,
+// and of one key's slots the first ones stay.  Then the slots in order: which become free below n_keep, which move; the places in
+// the lists of moves by one prefix sum.
 constexpr int kEvThreads = 1024;
-constexpr int kEvBins = 2048;
+constexpr int kEvWaves = kEvThreads / kWave;
+constexpr int kEvBins = 4096;
+constexpr int kEvStep = 256;          // slots of a wave at a time
+constexpr int kEvChunk = kEvStep * kEvWaves;
+constexpr int kEvMembers = 256;
+constexpr int kEvFew = 8;
+constexpr int kEvFused = 64;          // moves of a list that its workgroup makes itself
 
 struct EvictArgs {
     const int32_t* q_pos;
     int32_t* pos;
     float* weights;
     int32_t *src, *moves, *from, *to;   // moves [rows]: rows to move, -1 for none and no change of the length; from, to [rows, move_cap]
-    int lists, n_keep, n_sink, n_recent, move_cap;
+    uint32_t* count;                    // [B], zero between launches
+    int lists, n_keep, n_sink, n_recent, move_cap, D;
+    int fused;                          // no list has more than kEvFused moves: no second launch
 };
 
 // what a slot is ranked by: NaN below all weights, protected ones above all
+constexpr uint32_t kEvNan = 0u, kEvProtected = 0xffffffffu;
 __device__ __forceinline__ uint32_t evict_key(float w, int32_t p, int32_t n_sink, int64_t recent_from)
 {
-    return p < n_sink || (int64_t)p > recent_from ? 0xffffffffu : w != w ? 0u : score_key(w);
+    return p < n_sink || (int64_t)p > recent_from ? kEvProtected : w != w ? kEvNan : score_key(w);
 }
 
-// exclusive prefix sum over the workgroup's 16 waves; a barrier inside, another one before the next call's
-__device__ __forceinline__ uint32_t evict_scan(uint32_t v, uint32_t* sums, uint32_t* total)
+// One wave makes `n` <= 64 moves of a list: rows of K and V (the list's part of them), positions and weights.
+template <typename T>
+__device__ __forceinline__ void evict_move(const PagedCache& a, const EvictArgs& e, T* Kp, T* Vp, int rowi, const int32_t* from, const int32_t* to, int n)
 {
-    const int lane = lane_id(), wave = threadIdx.x >> 6;
-    const uint32_t iv = wave_incl_scan(v);
-    __syncthreads();
-    if (lane == kWave - 1) sums[wave] = iv;
-    __syncthreads();
+    constexpr int VEC = elem<T>::vec;
+    const int lane = lane_id(), b = idiv(rowi, e.lists), list = rowi - b * e.lists, row = a.H_kv * e.D;
+    int64_t x = -1, y = -1;   // lane k: move k
+    if (lane < n) {
+        const int f = from[lane], t = to[lane];
+        x = paged_row(a, b, f, row);
+        y = paged_row(a, b, t, row);
+        const size_t r = (size_t)rowi * a.cap;
+        const int32_t p = e.pos[r + f];
+        const float w = e.weights[r + f];
+        e.pos[r + t] = p;
+        e.weights[r + t] = w;
+        if (e.src) e.src[(size_t)rowi * e.n_keep + t] = f;
+        if (x < 0 || y < 0) x = y = -1;   // a page that is not there
+        else if (e.lists > 1) { x += list * e.D; y += list * e.D; }
+    }
+    const int pieces = (e.lists > 1 ? e.D : row) / VEC;   // of 16 bytes: 8, 16 or 32, or a whole row's
+    const int side = pieces < kWave ? idiv(kWave, pieces) : 1, my = idiv(lane, min(pieces, kWave)), first = lane - my * min(pieces, kWave);   // moves side by side
+    for (int m = 0; m < n; m += 4 * side)
+        for (int c0 = 0; c0 < pieces; c0 += kWave) {
+            const int c = c0 + first;
+            u32x4 k[4], v[4];
+            int64_t ys[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = m + u * side + my;
+                const int64_t xs = __shfl(x, min(i, kWave - 1));
+                ys[u] = __shfl(y, min(i, kWave - 1));
+                if (i >= n || my >= side || c >= pieces) ys[u] = -1;
+                if (ys[u] >= 0) {
+                    k[u] = ld16(Kp + xs + c * VEC);
+                    v[u] = ld16(Vp + xs + c * VEC);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (ys[u] >= 0) {
+                    *reinterpret_cast<u32x4*>(Kp + ys[u] + c * VEC) = k[u];
+                    *reinterpret_cast<u32x4*>(Vp + ys[u] + c * VEC) = v[u];
+                }
+        }
+}
+
+// exclusive prefix sum over the 16 waves' values (uniform in a wave) and the total, from LDS
+__device__ __forceinline__ uint32_t evict_before(const uint32_t* sums, int wave, uint32_t* total)
+{
+    const int lane = lane_id();
     const uint32_t w = sums[lane & 15];
-    *total = row16_sum_u32(w);
-    return row16_sum_u32((lane & 15) < wave ? w : 0u) + iv - v;
+    *total = wave_uniform((int)row16_sum_u32(w));
+    return wave_uniform((int)row16_sum_u32((lane & 15) < wave ? w : 0u));
 }
 
-// One workgroup per list: radix select over the 32-bit keys (11 + 11 + 10 bits) for the key of the n_keep-th slot, then the slots
-// in order: which stay, which become free below n_keep, which move.
-__global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCache a, EvictArgs e)
+// NC: steps of a wave in registers, 0: any number, read anew.  grid (B * lists)
+template <typename T, int NC>
+__global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len)
 {
-    __shared__ uint32_t hist[kEvBins];
-    __shared__ uint32_t sums[16];
-    __shared__ uint32_t sPrefix, sNeed;
-    const int rowi = blockIdx.x, b = rowi / e.lists, tid = threadIdx.x;
-    const int S = min(max(a.seq_len[b], 0), a.cap);
+    constexpr int NR = NC > 0 ? NC : 4;
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kEvBins];
+    __shared__ uint32_t sumA[2][kEvWaves], sumB[2][kEvWaves];
+    __shared__ uint32_t sKey[kEvMembers], sMembers;
+    __shared__ int32_t sSlot[kEvMembers];
+    __shared__ uint32_t sBin[3];
+    __shared__ int32_t sFrom[kEvFused], sTo[kEvFused];
+    const int rowi = blockIdx.x, b = idiv(rowi, e.lists), tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
+    const float* w = e.weights + (size_t)rowi * a.cap;
+    const int32_t* p = e.pos + (size_t)rowi * a.cap;
+    const int steps = (a.cap + kEvChunk - 1) / kEvChunk, slot0 = wave * steps * kEvStep + lane * 4;
+
+    // (a list need not begin on 16 bytes)
+    typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    typedef int32_t i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    struct Raw { f32x4 w; i32x4u p; };
+    auto load4 = [&](int c, Raw& r) {
+        const int j = slot0 + c * kEvStep;
+        if (j + 4 <= a.cap) {
+            r.w = *reinterpret_cast<const f32x4u*>(w + j);
+            r.p = *reinterpret_cast<const i32x4u*>(p + j);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { r.w[u] = j + u < a.cap ? w[j + u] : 0.f; r.p[u] = j + u < a.cap ? p[j + u] : 0; }
+        }
+    };
+    // requested with the length; what lies behind it is dropped later
+    Raw raw[NR];
+    if constexpr (NC > 0) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (c < steps) load4(c, raw[c]);
+    }
+    const int S = min(max(seq_len[b], 0), a.cap);
+    const int64_t recent_from = (int64_t)e.q_pos[b] - e.n_recent;
     int32_t* src = e.src ? e.src + (size_t)rowi * e.n_keep : nullptr;
     if (S <= e.n_keep) {
         if (src)
             for (int j = tid; j < e.n_keep; j += kEvThreads) src[j] = j < S ? j : -1;
-        if (tid == 0) e.moves[rowi] = -1;
+        if (tid == 0 && !e.fused) e.moves[rowi] = -1;
+        // (nobody counts on this list's arrival: the others of the sequence end here too)
         return;
     }
-    const float* w = e.weights + (size_t)rowi * a.cap;
-    const int32_t* p = e.pos + (size_t)rowi * a.cap;
-    const int64_t recent_from = (int64_t)e.q_pos[b] - e.n_recent;
-    auto key_of = [&](int j) { return evict_key(w[j], p[j], e.n_sink, recent_from); };
-    uint32_t prefix = 0, need = (uint32_t)e.n_keep;   // of the slots whose leading bits equal the prefix, `need` stay
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
-        __syncthreads();
-        for (int j = tid; j < S; j += kEvThreads) {
-            const uint32_t k = key_of(j);
-            if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[k >> shift & ((1u << bits) - 1)], 1u);
-        }
-        __syncthreads();
-        // thread t holds bins kEvBins-1-2t and the one below: sums from the top
-        const uint32_t c0 = hist[kEvBins - 1 - 2 * tid], c1 = hist[kEvBins - 2 - 2 * tid];
-        uint32_t total;
-        const uint32_t above = evict_scan(c0 + c1, sums, &total);
-        if (above < need && need <= above + c0 + c1) {
-            const bool second = need > above + c0;
-            sPrefix = prefix << bits | (uint32_t)(kEvBins - 1 - 2 * tid - (second ? 1 : 0));
-            sNeed = need - above - (second ? c0 : 0);
-        }
-        __syncthreads();
-        prefix = sPrefix;
-        need = sNeed;
+    auto keys_of = [&](const Raw& r, uint32_t (&k)[4]) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = evict_key(r.w[u], r.p[u], e.n_sink, recent_from);
+    };
+    uint32_t kr[NR][4];
+    if constexpr (NC > 0) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) keys_of(raw[c], kr[c]);
     }
-    uint32_t ties = 0, n_free = 0, n_late = 0;
-    for (int base = 0; base < S; base += 4 * kEvThreads) {
-        uint32_t key[4];
-        uint32_t eq = 0;
-        for (int u = 0; u < 4; ++u) {
-            const int j = base + 4 * tid + u;
-            key[u] = j < S ? key_of(j) : 0u;
-            eq += j < S && key[u] == prefix;
+    // f(step, first slot of this lane, its four keys), in the order of the slots
+    auto visit = [&](auto f) {
+        if constexpr (NC > 0) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (c < steps) f(c, slot0 + c * kEvStep, kr[c]);   // uniform
+        } else {
+            for (int c0 = 0; c0 < steps && slot0 - lane * 4 + c0 * kEvStep < S; c0 += NR) {
+                Raw r[NR];
+#pragma unroll
+                for (int c = 0; c < NR; ++c)
+                    if (c0 + c < steps) load4(c0 + c, r[c]);
+#pragma unroll
+                for (int c = 0; c < NR; ++c)
+                    if (c0 + c < steps) {
+                        uint32_t k[4];
+                        keys_of(r[c], k);
+                        f(c0 + c, slot0 + (c0 + c) * kEvStep, k);
+                    }
+            }
         }
+    };
+
+    int32_t* const from = e.fused ? sFrom : e.from + (size_t)rowi * e.move_cap;
+    int32_t* const to = e.fused ? sTo : e.to + (size_t)rowi * e.move_cap;
+    auto make_moves = [&](int n) {   // every wave some of them
+        const int each = (n + kEvWaves - 1) / kEvWaves, m0 = wave * each, mine = min(each, n - m0);
+        if (mine > 0) evict_move<T>(a, e, Kp, Vp, rowi, sFrom + m0, sTo + m0, mine);
+    };
+    auto done = [&](int left) {      // moves that are left to the second launch; without one, the last of the sequence's lists sets the length
+        if (tid != 0) return;
+        if (!e.fused) e.moves[rowi] = left;
+        else if (e.lists == 1 || arrive(e.count + b, (uint32_t)e.lists) == (uint32_t)e.lists - 1) seq_len[b] = e.n_keep;
+    };
+
+    // ---- few leave: the lowest, one by one ----
+    if constexpr (NC > 0)
+        if (S - e.n_keep <= kEvFew) {
+            const int n_out = S - e.n_keep;
+            if (src)
+                for (int j = tid; j < e.n_keep; j += kEvThreads) src[j] = j;   // (the moves' are written behind them)
+            uint32_t last = 0;
+            int last_slot = 0x7fffffff, out = -1;   // lane i: the slot that left in round i
+            for (int r = 0; r < n_out; ++r) {
+                uint32_t low = 0xffffffffu;
+                int at = -1;
+                visit([&](int, int j0, const uint32_t (&k)[4]) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int j = j0 + u;
+                        if (j < S && (k[u] > last || (k[u] == last && j < last_slot)) && (k[u] < low || (k[u] == low && j > at))) { low = k[u]; at = j; }
+                    }
+                });
+                const uint32_t wl = wave_min_u32(low);
+                const uint32_t ws = wave_max_u32(low == wl ? (uint32_t)(at + 1) : 0u);
+                if (lane == 0) { sumA[r & 1][wave] = wl; sumB[r & 1][wave] = ws; }
+                __syncthreads();
+                const uint32_t al = sumA[r & 1][lane & 15], as = sumB[r & 1][lane & 15];
+                last = wave_min_u32(al);
+                last_slot = (int)wave_max_u32(al == last ? as : 0u) - 1;
+                if (lane == r) out = last_slot;
+            }
+            const bool left = lane < n_out, fr = left && out < e.n_keep;
+            bool late = left;            // slot n_keep + lane, unless it is among those that left
+            int rank = 0;
+            for (int i = 0; i < n_out; ++i) {
+                const int o = __builtin_amdgcn_readlane(out, i);
+                rank += o < out;
+                late = late && o != e.n_keep + lane;
+            }
+            const uint64_t late_of = __ballot(late);
+            if (wave == 0) {
+                if (fr) sTo[rank] = out;
+                if (late) sFrom[__popcll(late_of & ((1ull << lane) - 1))] = e.n_keep + lane;
+            }
+            __syncthreads();
+            make_moves(__popcll(late_of));
+            done(0);
+            return;
+        }
+
+    // ---- threshold: what is above (key, slot) stays, as do that key's slots up to that slot ----
+    uint32_t key = 0, need = (uint32_t)e.n_keep, members = (uint32_t)S;
+    int slot = 0x7fffffff;
+    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
+    if (tid == 0) sMembers = 0;
+    __syncthreads();
+    for (int shift = 20, bits = 12;;) {
+        visit([&](int, int j0, const uint32_t (&k)[4]) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool on = j0 + u < S && (shift == 20 || k[u] >> (shift + bits) == key);
+                const uint32_t bin = k[u] >> shift & ((1u << bits) - 1);
+                // lanes with the first one's bin count together: weights that are all alike would queue up at one address
+                const uint64_t act = __ballot(on);
+                if (act) {
+                    const int first = __ffsll((unsigned long long)act) - 1;
+                    const bool same = on && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, first);
+                    const uint32_t n = (uint32_t)__popcll(__ballot(same));
+                    if (on && (!same || lane == first)) atomicAdd(&hist[bin], same ? n : 1u);
+                }
+            }
+        });
+        __syncthreads();
+        // thread t: the four bins from 4 (1023 - t) on, the upper ones first
+        const u32x4 h = *reinterpret_cast<const u32x4*>(&hist[4 * (kEvThreads - 1 - tid)]);
+        const uint32_t four = h.x + h.y + h.z + h.w, upto = wave_incl_scan(four);
+        if (lane == kWave - 1) sumA[0][wave] = upto;
+        __syncthreads();
         uint32_t total;
-        uint32_t rank = ties + evict_scan(eq, sums, &total);
-        ties += total;
-        uint32_t mine = 0;   // free slots, and moving ones in the upper half
-        int what[4];
+        uint32_t above = evict_before(sumA[0], wave, &total) + upto - four;
+        if (above < need && need <= above + four) {
+            int u = 3;
+            for (; need > above + h[u]; --u) above += h[u];
+            sBin[0] = 4u * (uint32_t)(kEvThreads - 1 - tid) + (uint32_t)u;
+            sBin[1] = need - above;
+            sBin[2] = h[u];
+        }
+        *reinterpret_cast<u32x4*>(&hist[4 * (kEvThreads - 1 - tid)]) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+        key = key << bits | sBin[0];
+        need = sBin[1];
+        members = sBin[2];
+        if (need == members) { key = (key << shift) - 1u; slot = -1; break; }   // the bin stays whole (bin 0 cannot: then all would)
+        if (members <= (uint32_t)kEvMembers || shift == 0) {
+            const uint32_t bin_key = key;
+            if (members <= (uint32_t)kEvMembers) {
+                visit([&](int, int j0, const uint32_t (&k)[4]) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (j0 + u < S && k[u] >> shift == bin_key) {
+                            const uint32_t i = atomicAdd(&sMembers, 1u);
+                            sKey[i] = k[u];
+                            sSlot[i] = j0 + u;
+                        }
+                });
+                __syncthreads();
+                // four threads for each member
+                const int i = tid >> 2, part = tid & 3;
+                uint32_t before = 0;
+                if (i < (int)members)
+                    for (int o = part; o < (int)members; o += 4) before += sKey[o] > sKey[i] || (sKey[o] == sKey[i] && sSlot[o] < sSlot[i]);
+                before += __shfl_xor((int)before, 1);
+                before += __shfl_xor((int)before, 2);
+                if (i < (int)members && part == 0 && before == need - 1) { sBin[0] = sKey[i]; sBin[1] = (uint32_t)sSlot[i]; }
+            } else {   // many slots of one key: the need-th of them
+                uint32_t mine = 0;
+                visit([&](int, int j0, const uint32_t (&k)[4]) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) mine += j0 + u < S && k[u] == bin_key;
+                });
+                mine = wave_sum_u32(mine);
+                if (lane == 0) sumB[0][wave] = mine;
+                __syncthreads();
+                uint32_t run = evict_before(sumB[0], wave, &total);
+                if (run < need && need <= run + mine)   // (one wave)
+                    visit([&](int, int j0, const uint32_t (&k)[4]) {
+                        uint32_t n = 0;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) n += j0 + u < S && k[u] == bin_key;
+                        const uint32_t incl = wave_incl_scan(n);
+                        uint32_t r = run + incl - n;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (j0 + u < S && k[u] == bin_key && ++r == need) { sBin[0] = bin_key; sBin[1] = (uint32_t)(j0 + u); }
+                        run += (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
+                    });
+            }
+            __syncthreads();
+            key = sBin[0];
+            slot = (int)sBin[1];
+            break;
+        }
+        if (shift == 20) shift = 8;
+        else { shift = 0; bits = 8; }
+    }
+
+    // ---- the slots in order ----
+    auto kinds = [&](int j0, const uint32_t (&k)[4], bool (&fr)[4], bool (&lt)[4]) {
+#pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int j = base + 4 * tid + u;
-            const bool tie = j < S && key[u] == prefix;
-            const bool kept = j < S && (key[u] > prefix || (tie && rank < need));
-            rank += tie;
-            what[u] = j >= S || kept == (j < e.n_keep) ? 0 : kept ? 2 : 1;
-            mine += what[u] == 1 ? 1u : what[u] == 2 ? 0x10000u : 0u;
+            const int j = j0 + u;
+            const bool kept = j < S && (k[u] > key || (k[u] == key && j <= slot));
+            fr[u] = j < S && !kept && j < e.n_keep;
+            lt[u] = kept && j >= e.n_keep;
             if (src && kept && j < e.n_keep) src[j] = j;
         }
-        const uint32_t before = evict_scan(mine, sums, &total);
-        uint32_t f = n_free + (before & 0xffffu), m = n_late + (before >> 16);
-        n_free += total & 0xffffu;
-        n_late += total >> 16;
+    };
+    uint32_t frees = 0, lates = 0;   // of the wave
+    visit([&](int, int j0, const uint32_t (&k)[4]) {
+#pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int j = base + 4 * tid + u;
-            if (what[u] == 1) e.to[(size_t)rowi * e.move_cap + f++] = j;
-            if (what[u] == 2) e.from[(size_t)rowi * e.move_cap + m++] = j;
+            const int j = j0 + u;
+            const bool kept = j < S && (k[u] > key || (k[u] == key && j <= slot));
+            frees += (uint32_t)__popcll(__ballot(j < S && !kept && j < e.n_keep));
+            lates += (uint32_t)__popcll(__ballot(kept && j >= e.n_keep));
         }
+    });
+    if (lane == 0) { sumA[1][wave] = frees; sumB[1][wave] = lates; }
+    __syncthreads();
+    uint32_t n_free, n_late;
+    uint32_t f0 = evict_before(sumA[1], wave, &n_free), l0 = evict_before(sumB[1], wave, &n_late);
+    visit([&](int, int j0, const uint32_t (&k)[4]) {
+        bool fr[4], lt[4];
+        kinds(j0, k, fr, lt);
+        uint32_t n = 0;   // free, and moving in the upper half
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += fr[u] ? 1u : lt[u] ? 0x10000u : 0u;
+        const uint32_t incl = wave_incl_scan(n), tot = (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
+        uint32_t f = f0 + ((incl - n) & 0xffffu), l = l0 + ((incl - n) >> 16);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (fr[u]) to[f++] = j0 + u;
+            if (lt[u]) from[l++] = j0 + u;
+        }
+        f0 += tot & 0xffffu;
+        l0 += tot >> 16;
+    });
+    if (!e.fused) {
+        done((int)n_free);
+        return;
     }
-    if (tid == 0) e.moves[rowi] = (int32_t)n_free;
+    __syncthreads();
+    make_moves((int)n_free);
+    done(0);
 }
 
-// grid (x, rows): the rows of K and V, positions and weights of the moving slots; then the length
+// grid (x, rows): the moves, `batch` of them a wave at a time; then the length
 template <typename T>
-__global__ __launch_bounds__(256) void paged_evict_move_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len,
-                                                               int D)
+__global__ __launch_bounds__(256) void paged_evict_move_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len, int batch)
 {
-    constexpr int VEC = elem<T>::vec;
-    const int rowi = blockIdx.y, b = rowi / e.lists, list = rowi % e.lists, row = a.H_kv * D;
+    const int rowi = blockIdx.y, b = idiv(rowi, e.lists), wave = wave_uniform((int)threadIdx.x >> 6);
     const int n = e.moves[rowi];
     if (n < 0) return;
-    if (blockIdx.x == 0 && list == 0 && threadIdx.x == 0) seq_len[b] = e.n_keep;
+    if (blockIdx.x == 0 && rowi == b * e.lists && threadIdx.x == 0) seq_len[b] = e.n_keep;
     const int32_t *from = e.from + (size_t)rowi * e.move_cap, *to = e.to + (size_t)rowi * e.move_cap;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-        const size_t r = (size_t)rowi * a.cap;
-        e.pos[r + to[i]] = e.pos[r + from[i]];
-        e.weights[r + to[i]] = e.weights[r + from[i]];
-        if (e.src) e.src[(size_t)rowi * e.n_keep + to[i]] = from[i];
-    }
-    const int pieces = (e.lists == 1 ? row : D) / VEC, off = e.lists == 1 ? 0 : list * D;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * pieces; i += (int64_t)gridDim.x * 256) {
-        const int m = (int)(i / pieces), pc = (int)(i - (int64_t)m * pieces);
-        const int64_t x = paged_row(a, b, from[m], row), y = paged_row(a, b, to[m], row);
-        if (x < 0 || y < 0) continue;
-        const int64_t o = off + pc * VEC;
-        const u32x4 k = ld16(Kp + x + o), v = ld16(Vp + x + o);
-        *reinterpret_cast<u32x4*>(Kp + y + o) = k;
-        *reinterpret_cast<u32x4*>(Vp + y + o) = v;
-    }
+    for (int m = (blockIdx.x * 4 + wave) * batch; m < n; m += gridDim.x * 4 * batch) evict_move<T>(a, e, Kp, Vp, rowi, from + m, to + m, min(batch, n - m));
 }
 
 __global__ __launch_bounds__(256) void paged_clear_kernel(uint32_t* count, int n)

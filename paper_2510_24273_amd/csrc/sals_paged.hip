@@ -157,12 +157,21 @@ sals_status launch_evict(const sals_paged* c, const int32_t* q_pos, const int32_
     EvictArgs e;
     e.q_pos = q_pos; e.pos = pos; e.weights = weights; e.src = src;
     e.moves = at<int32_t>(c, c->L.moves); e.from = at<int32_t>(c, c->L.from); e.to = at<int32_t>(c, c->L.to);
-    e.lists = d.weight_heads; e.n_keep = n_keep; e.n_sink = n_sink; e.n_recent = n_recent; e.move_cap = c->L.move_cap;
-    const int rows = d.B * d.weight_heads;
-    hipLaunchKernelGGL(paged_evict_select_kernel, dim3(rows), dim3(kEvThreads), 0, st, a, e);
-    if (launch_status() != SALS_OK) return SALS_ERR_HIP;
-    const int x = std::max(1, std::min(2048 / rows, ceil_div(std::min(n_keep, a.cap - n_keep), 16)));
-    hipLaunchKernelGGL((paged_evict_move_kernel<T>), dim3(x, rows), dim3(256), 0, st, a, e, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len, d.d);
+    e.count = at<uint32_t>(c, c->L.count);
+    e.lists = d.weight_heads; e.n_keep = n_keep; e.n_sink = n_sink; e.n_recent = n_recent; e.move_cap = c->L.move_cap; e.D = d.d;
+    const int rows = d.B * d.weight_heads, most = std::min(n_keep, a.cap - n_keep);   // moves of a list
+    e.fused = most <= kEvFused;
+    auto select = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(rows), dim3(kEvThreads), 0, st, a, e, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len);
+    };
+    if (a.cap <= kEvChunk) select(paged_evict_select_kernel<T, 1>);
+    else if (a.cap <= 2 * kEvChunk) select(paged_evict_select_kernel<T, 2>);
+    else if (a.cap <= 8 * kEvChunk) select(paged_evict_select_kernel<T, 8>);
+    else select(paged_evict_select_kernel<T, 0>);
+    if (launch_status() != SALS_OK || e.fused) return launch_status();
+    // whole rows: eight moves a wave, a head's part of them: 16
+    const int batch = e.lists == 1 && d.H_kv > 1 ? 8 : 16, x = std::max(1, std::min(ceil_div(4096, rows), ceil_div(most, 4 * batch)));
+    hipLaunchKernelGGL((paged_evict_move_kernel<T>), dim3(x, rows), dim3(256), 0, st, a, e, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len, batch);
     return launch_status();
 }
 
