@@ -646,7 +646,7 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------
 // A list's n_keep slots of the largest keys, and the moves that bring them below slot n_keep.  One workgroup per list; a wave holds
-// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps; longer lists are read anew in every pass.
+// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps (32768 slots; longer lists, and few of more than 16384 slots, further below).
 //
 // Threshold: the key and the slot of the last one that stays.  Where up to kEvFew leave they are found one by one (the lowest first).
 // Otherwise a histogram over the keys' leading 12 bits (keys are the floats' bits in order, so eight bins for a factor of two) names the
@@ -735,42 +735,96 @@ __device__ __forceinline__ uint32_t evict_before(const uint32_t* sums, int wave,
     return wave_uniform((int)row16_sum_u32((lane & 15) < wave ? w : 0u));
 }
 
-// NC: steps of a wave in registers, 0: any number, read anew.  grid (B * lists)
+struct EvictShared {
+    __attribute__((aligned(16))) uint32_t hist[kEvBins];
+    uint32_t sumA[2][kEvWaves], sumB[2][kEvWaves];
+    uint32_t key[kEvMembers], n_members;
+    int32_t slot[kEvMembers];
+    uint32_t bin[3];
+    int32_t from[kEvFused], to[kEvFused];
+    uint32_t last;
+};
+
+// weights and positions of four slots from j on (a list need not begin on 16 bytes); what lies behind the list is zero
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+struct EvictRaw {
+    f32x4 w;
+    i32x4u p;
+    __device__ __forceinline__ void load(const float* weights, const int32_t* pos, int j, int cap)
+    {
+        if (j + 4 <= cap) {
+            w = *reinterpret_cast<const f32x4u*>(weights + j);
+            p = *reinterpret_cast<const i32x4u*>(pos + j);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { w[u] = j + u < cap ? weights[j + u] : 0.f; p[u] = j + u < cap ? pos[j + u] : 0; }
+        }
+    }
+    __device__ __forceinline__ void keys(uint32_t (&k)[4], int32_t n_sink, int64_t recent_from) const
+    {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = evict_key(w[u], p[u], n_sink, recent_from);
+    }
+};
+
+// Counts of a bin in LDS; lanes with the first one's bin count together: weights that are all alike would queue up at one address.
+__device__ __forceinline__ void evict_count(uint32_t* hist, uint32_t bin, bool on)
+{
+    const uint64_t act = __ballot(on);
+    if (!act) return;
+    const int lane = lane_id(), first = __ffsll((unsigned long long)act) - 1;
+    const bool same = on && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, first);
+    const uint32_t n = (uint32_t)__popcll(__ballot(same));
+    if (on && (!same || lane == first)) atomicAdd(&hist[bin], same ? n : 1u);
+}
+
+// Of the 4096 bins, of which this thread holds h = those from 4 (1023 - t) on: the one that the `need`-th largest is in, how many of
+// its members are needed and how many it has, left in sh.bin (two barriers inside, the second one behind the result).
+__device__ __forceinline__ void evict_bin(EvictShared& sh, const u32x4& h, uint32_t need)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
+    const uint32_t four = h.x + h.y + h.z + h.w, upto = wave_incl_scan(four);
+    if (lane == kWave - 1) sh.sumA[0][wave] = upto;
+    __syncthreads();
+    uint32_t total, above = evict_before(sh.sumA[0], wave, &total) + upto - four;
+    if (above < need && need <= above + four) {
+        int u = 3;
+        for (; need > above + h[u]; --u) above += h[u];
+        sh.bin[0] = 4u * (uint32_t)(kEvThreads - 1 - tid) + (uint32_t)u;
+        sh.bin[1] = need - above;
+        sh.bin[2] = h[u];
+    }
+    __syncthreads();
+}
+
+// The need-th of n <= kEvMembers members in sh.key, sh.slot by rank, left in sh.bin[0], sh.bin[1]: four threads for each
+__device__ __forceinline__ void evict_rank(EvictShared& sh, int n, uint32_t need)
+{
+    const int i = threadIdx.x >> 2, part = threadIdx.x & 3;
+    uint32_t before = 0;
+    if (i < n)
+        for (int o = part; o < n; o += 4) before += sh.key[o] > sh.key[i] || (sh.key[o] == sh.key[i] && sh.slot[o] < sh.slot[i]);
+    before += (uint32_t)__shfl_xor((int)before, 1);
+    before += (uint32_t)__shfl_xor((int)before, 2);
+    if (i < n && part == 0 && before == need - 1) { sh.bin[0] = sh.key[i]; sh.bin[1] = (uint32_t)sh.slot[i]; }
+}
+
+// One list by the calling workgroup.  NC: steps of a wave in registers, 0: any number, read anew (then e.fused must be 0)
 template <typename T, int NC>
-__global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len)
+__device__ __forceinline__ void evict_select(EvictShared& sh, const PagedCache& a, const EvictArgs& e, T* Kp, T* Vp, int32_t* seq_len, int rowi)
 {
     constexpr int NR = NC > 0 ? NC : 4;
-    __shared__ __attribute__((aligned(16))) uint32_t hist[kEvBins];
-    __shared__ uint32_t sumA[2][kEvWaves], sumB[2][kEvWaves];
-    __shared__ uint32_t sKey[kEvMembers], sMembers;
-    __shared__ int32_t sSlot[kEvMembers];
-    __shared__ uint32_t sBin[3];
-    __shared__ int32_t sFrom[kEvFused], sTo[kEvFused];
-    const int rowi = blockIdx.x, b = idiv(rowi, e.lists), tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
+    const int b = idiv(rowi, e.lists), tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
     const float* w = e.weights + (size_t)rowi * a.cap;
     const int32_t* p = e.pos + (size_t)rowi * a.cap;
     const int steps = (a.cap + kEvChunk - 1) / kEvChunk, slot0 = wave * steps * kEvStep + lane * 4;
-
-    // (a list need not begin on 16 bytes)
-    typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-    typedef int32_t i32x4u __attribute__((ext_vector_type(4), aligned(4)));
-    struct Raw { f32x4 w; i32x4u p; };
-    auto load4 = [&](int c, Raw& r) {
-        const int j = slot0 + c * kEvStep;
-        if (j + 4 <= a.cap) {
-            r.w = *reinterpret_cast<const f32x4u*>(w + j);
-            r.p = *reinterpret_cast<const i32x4u*>(p + j);
-        } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { r.w[u] = j + u < a.cap ? w[j + u] : 0.f; r.p[u] = j + u < a.cap ? p[j + u] : 0; }
-        }
-    };
     // requested with the length; what lies behind it is dropped later
-    Raw raw[NR];
+    EvictRaw raw[NR];
     if constexpr (NC > 0) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
-            if (c < steps) load4(c, raw[c]);
+            if (c < steps) raw[c].load(w, p, slot0 + c * kEvStep, a.cap);
     }
     const int S = min(max(seq_len[b], 0), a.cap);
     const int64_t recent_from = (int64_t)e.q_pos[b] - e.n_recent;
@@ -782,14 +836,10 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
         // (nobody counts on this list's arrival: the others of the sequence end here too)
         return;
     }
-    auto keys_of = [&](const Raw& r, uint32_t (&k)[4]) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = evict_key(r.w[u], r.p[u], e.n_sink, recent_from);
-    };
     uint32_t kr[NR][4];
     if constexpr (NC > 0) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) keys_of(raw[c], kr[c]);
+        for (int c = 0; c < NC; ++c) raw[c].keys(kr[c], e.n_sink, recent_from);
     }
     // f(step, first slot of this lane, its four keys), in the order of the slots
     auto visit = [&](auto f) {
@@ -799,26 +849,26 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
                 if (c < steps) f(c, slot0 + c * kEvStep, kr[c]);   // uniform
         } else {
             for (int c0 = 0; c0 < steps && slot0 - lane * 4 + c0 * kEvStep < S; c0 += NR) {
-                Raw r[NR];
+                EvictRaw r[NR];
 #pragma unroll
                 for (int c = 0; c < NR; ++c)
-                    if (c0 + c < steps) load4(c0 + c, r[c]);
+                    if (c0 + c < steps) r[c].load(w, p, slot0 + (c0 + c) * kEvStep, a.cap);
 #pragma unroll
                 for (int c = 0; c < NR; ++c)
                     if (c0 + c < steps) {
                         uint32_t k[4];
-                        keys_of(r[c], k);
+                        r[c].keys(k, e.n_sink, recent_from);
                         f(c0 + c, slot0 + (c0 + c) * kEvStep, k);
                     }
             }
         }
     };
 
-    int32_t* const from = e.fused ? sFrom : e.from + (size_t)rowi * e.move_cap;
-    int32_t* const to = e.fused ? sTo : e.to + (size_t)rowi * e.move_cap;
+    int32_t* const from = e.fused ? sh.from : e.from + (size_t)rowi * e.move_cap;
+    int32_t* const to = e.fused ? sh.to : e.to + (size_t)rowi * e.move_cap;
     auto make_moves = [&](int n) {   // every wave some of them
         const int each = (n + kEvWaves - 1) / kEvWaves, m0 = wave * each, mine = min(each, n - m0);
-        if (mine > 0) evict_move<T>(a, e, Kp, Vp, rowi, sFrom + m0, sTo + m0, mine);
+        if (mine > 0) evict_move<T>(a, e, Kp, Vp, rowi, sh.from + m0, sh.to + m0, mine);
     };
     auto done = [&](int left) {      // moves that are left to the second launch; without one, the last of the sequence's lists sets the length
         if (tid != 0) return;
@@ -846,9 +896,9 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
                 });
                 const uint32_t wl = wave_min_u32(low);
                 const uint32_t ws = wave_max_u32(low == wl ? (uint32_t)(at + 1) : 0u);
-                if (lane == 0) { sumA[r & 1][wave] = wl; sumB[r & 1][wave] = ws; }
+                if (lane == 0) { sh.sumA[r & 1][wave] = wl; sh.sumB[r & 1][wave] = ws; }
                 __syncthreads();
-                const uint32_t al = sumA[r & 1][lane & 15], as = sumB[r & 1][lane & 15];
+                const uint32_t al = sh.sumA[r & 1][lane & 15], as = sh.sumB[r & 1][lane & 15];
                 last = wave_min_u32(al);
                 last_slot = (int)wave_max_u32(al == last ? as : 0u) - 1;
                 if (lane == r) out = last_slot;
@@ -863,8 +913,8 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
             }
             const uint64_t late_of = __ballot(late);
             if (wave == 0) {
-                if (fr) sTo[rank] = out;
-                if (late) sFrom[__popcll(late_of & ((1ull << lane) - 1))] = e.n_keep + lane;
+                if (fr) sh.to[rank] = out;
+                if (late) sh.from[__popcll(late_of & ((1ull << lane) - 1))] = e.n_keep + lane;
             }
             __syncthreads();
             make_moves(__popcll(late_of));
@@ -875,45 +925,23 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
     // ---- threshold: what is above (key, slot) stays, as do that key's slots up to that slot ----
     uint32_t key = 0, need = (uint32_t)e.n_keep, members = (uint32_t)S;
     int slot = 0x7fffffff;
-    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
-    if (tid == 0) sMembers = 0;
+    for (int i = tid; i < kEvBins; i += kEvThreads) sh.hist[i] = 0;
+    if (tid == 0) sh.n_members = 0;
     __syncthreads();
     for (int shift = 20, bits = 12;;) {
         visit([&](int, int j0, const uint32_t (&k)[4]) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const bool on = j0 + u < S && (shift == 20 || k[u] >> (shift + bits) == key);
-                const uint32_t bin = k[u] >> shift & ((1u << bits) - 1);
-                // lanes with the first one's bin count together: weights that are all alike would queue up at one address
-                const uint64_t act = __ballot(on);
-                if (act) {
-                    const int first = __ffsll((unsigned long long)act) - 1;
-                    const bool same = on && bin == (uint32_t)__builtin_amdgcn_readlane((int)bin, first);
-                    const uint32_t n = (uint32_t)__popcll(__ballot(same));
-                    if (on && (!same || lane == first)) atomicAdd(&hist[bin], same ? n : 1u);
-                }
-            }
+            for (int u = 0; u < 4; ++u)
+                evict_count(sh.hist, k[u] >> shift & ((1u << bits) - 1), j0 + u < S && (shift == 20 || k[u] >> (shift + bits) == key));
         });
         __syncthreads();
-        // thread t: the four bins from 4 (1023 - t) on, the upper ones first
-        const u32x4 h = *reinterpret_cast<const u32x4*>(&hist[4 * (kEvThreads - 1 - tid)]);
-        const uint32_t four = h.x + h.y + h.z + h.w, upto = wave_incl_scan(four);
-        if (lane == kWave - 1) sumA[0][wave] = upto;
-        __syncthreads();
-        uint32_t total;
-        uint32_t above = evict_before(sumA[0], wave, &total) + upto - four;
-        if (above < need && need <= above + four) {
-            int u = 3;
-            for (; need > above + h[u]; --u) above += h[u];
-            sBin[0] = 4u * (uint32_t)(kEvThreads - 1 - tid) + (uint32_t)u;
-            sBin[1] = need - above;
-            sBin[2] = h[u];
-        }
-        *reinterpret_cast<u32x4*>(&hist[4 * (kEvThreads - 1 - tid)]) = u32x4{0u, 0u, 0u, 0u};
-        __syncthreads();
-        key = key << bits | sBin[0];
-        need = sBin[1];
-        members = sBin[2];
+        u32x4* const four = reinterpret_cast<u32x4*>(&sh.hist[4 * (kEvThreads - 1 - tid)]);
+        const u32x4 h = *four;
+        *four = u32x4{0u, 0u, 0u, 0u};
+        evict_bin(sh, h, need);
+        key = key << bits | sh.bin[0];
+        need = sh.bin[1];
+        members = sh.bin[2];
         if (need == members) { key = (key << shift) - 1u; slot = -1; break; }   // the bin stays whole (bin 0 cannot: then all would)
         if (members <= (uint32_t)kEvMembers || shift == 0) {
             const uint32_t bin_key = key;
@@ -922,20 +950,13 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         if (j0 + u < S && k[u] >> shift == bin_key) {
-                            const uint32_t i = atomicAdd(&sMembers, 1u);
-                            sKey[i] = k[u];
-                            sSlot[i] = j0 + u;
+                            const uint32_t i = atomicAdd(&sh.n_members, 1u);
+                            sh.key[i] = k[u];
+                            sh.slot[i] = j0 + u;
                         }
                 });
                 __syncthreads();
-                // four threads for each member
-                const int i = tid >> 2, part = tid & 3;
-                uint32_t before = 0;
-                if (i < (int)members)
-                    for (int o = part; o < (int)members; o += 4) before += sKey[o] > sKey[i] || (sKey[o] == sKey[i] && sSlot[o] < sSlot[i]);
-                before += __shfl_xor((int)before, 1);
-                before += __shfl_xor((int)before, 2);
-                if (i < (int)members && part == 0 && before == need - 1) { sBin[0] = sKey[i]; sBin[1] = (uint32_t)sSlot[i]; }
+                evict_rank(sh, (int)members, need);
             } else {   // many slots of one key: the need-th of them
                 uint32_t mine = 0;
                 visit([&](int, int j0, const uint32_t (&k)[4]) {
@@ -943,9 +964,9 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
                     for (int u = 0; u < 4; ++u) mine += j0 + u < S && k[u] == bin_key;
                 });
                 mine = wave_sum_u32(mine);
-                if (lane == 0) sumB[0][wave] = mine;
+                if (lane == 0) sh.sumB[0][wave] = mine;
                 __syncthreads();
-                uint32_t run = evict_before(sumB[0], wave, &total);
+                uint32_t total, run = evict_before(sh.sumB[0], wave, &total);
                 if (run < need && need <= run + mine)   // (one wave)
                     visit([&](int, int j0, const uint32_t (&k)[4]) {
                         uint32_t n = 0;
@@ -955,13 +976,13 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
                         uint32_t r = run + incl - n;
 #pragma unroll
                         for (int u = 0; u < 4; ++u)
-                            if (j0 + u < S && k[u] == bin_key && ++r == need) { sBin[0] = bin_key; sBin[1] = (uint32_t)(j0 + u); }
+                            if (j0 + u < S && k[u] == bin_key && ++r == need) { sh.bin[0] = bin_key; sh.bin[1] = (uint32_t)(j0 + u); }
                         run += (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
                     });
             }
             __syncthreads();
-            key = sBin[0];
-            slot = (int)sBin[1];
+            key = sh.bin[0];
+            slot = (int)sh.bin[1];
             break;
         }
         if (shift == 20) shift = 8;
@@ -989,10 +1010,10 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
             lates += (uint32_t)__popcll(__ballot(kept && j >= e.n_keep));
         }
     });
-    if (lane == 0) { sumA[1][wave] = frees; sumB[1][wave] = lates; }
+    if (lane == 0) { sh.sumA[1][wave] = frees; sh.sumB[1][wave] = lates; }
     __syncthreads();
     uint32_t n_free, n_late;
-    uint32_t f0 = evict_before(sumA[1], wave, &n_free), l0 = evict_before(sumB[1], wave, &n_late);
+    uint32_t f0 = evict_before(sh.sumA[1], wave, &n_free), l0 = evict_before(sh.sumB[1], wave, &n_late);
     visit([&](int, int j0, const uint32_t (&k)[4]) {
         bool fr[4], lt[4];
         kinds(j0, k, fr, lt);
@@ -1018,6 +1039,292 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
     done(0);
 }
 
+// grid (B * lists)
+template <typename T, int NC>
+__global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len)
+{
+    __shared__ EvictShared sh;
+    evict_select<T, NC>(sh, a, e, Kp, Vp, seq_len, blockIdx.x);
+}
+
+// ---- longer lists: a workgroup for each 4096 slots, in three launches (a list's keys are too many instructions for one compute unit:
+// 4 x (82 000 of 4 lists) 47 us in one workgroup each) ----
+// hist     the chunks' histograms of the leading 12 bits added up for the list; the last chunk to arrive finds the bin
+// (split   lists of more than 131072 slots: the same with the next 12 bits, if the bin has more members than a workgroup ranks)
+// members  every chunk counts what is certain to become free or to move, and lists the bin's members; the last one ranks them and
+//          leaves the threshold and the chunks' places in the lists of moves.  A list with more members than that (one weight many times
+//          over) is done by that workgroup alone.
+// emit     every chunk writes its part of the lists of moves
+constexpr int kEvCand = 4096;
+constexpr int kEvMaxChunks = (1 << 20) / kEvChunk;
+enum { kEvKey = 0, kEvNeed, kEvCount, kEvShift, kEvSlot, kEvDone, kEvState = 8 };   // a list's state
+
+struct EvictChain {
+    uint32_t *hist, *n_cand, *arrived;   // [rows][kEvBins], [rows], [rows]: zero between launches
+    uint32_t* state;                     // [rows][kEvState]
+    uint2* cand;                         // [rows][kEvCand]: key, slot
+    uint2* part;                         // [rows][chunks]: free and moving slots of a chunk, then the places of its first ones
+    int chunks;                          // of a list's capacity
+};
+
+__device__ __forceinline__ uint32_t ldu_device(const uint32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint2 ldu2_device(const uint2* p)
+{
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_uint2((uint32_t)v, (uint32_t)(v >> 32));
+}
+__device__ __forceinline__ void stu2_device(uint2* p, uint32_t x, uint32_t y)
+{
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)y << 32 | x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// the calling chunk of a list: its keys, four for each thread
+struct EvictPiece {
+    int b, S, j0;
+    uint32_t k[4];
+    __device__ __forceinline__ EvictPiece(const PagedCache& a, const EvictArgs& e, const int32_t* seq_len, int rowi, int chunk)
+    {
+        b = idiv(rowi, e.lists);
+        j0 = chunk * kEvChunk + 4 * threadIdx.x;
+        EvictRaw r;
+        r.load(e.weights + (size_t)rowi * a.cap, e.pos + (size_t)rowi * a.cap, j0, a.cap);
+        S = min(max(seq_len[b], 0), a.cap);
+        r.keys(k, e.n_sink, (int64_t)e.q_pos[b] - e.n_recent);
+    }
+    __device__ __forceinline__ int live() const { return (S + kEvChunk - 1) / kEvChunk; }   // chunks that hold slots in use
+};
+
+// is this the last of the list's `n` chunks to arrive?  (for all threads; stores and atomics before are the device's by then)
+__device__ __forceinline__ bool evict_last(EvictShared& sh, uint32_t* count, int n)
+{
+    device_stores_done();
+    __syncthreads();
+    if (threadIdx.x == 0) sh.last = arrive(count, (uint32_t)n) == (uint32_t)n - 1;
+    __syncthreads();
+    return sh.last != 0;
+}
+
+// grid (chunks, rows)
+__global__ __launch_bounds__(kEvThreads) void paged_evict_hist_kernel(PagedCache a, EvictArgs e, EvictChain c, const int32_t* __restrict__ seq_len, int split)
+{
+    __shared__ EvictShared sh;
+    const int rowi = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x;
+    uint32_t* const st = c.state + (size_t)rowi * kEvState;
+    const uint32_t prefix = split ? st[kEvKey] : 0u;
+    if (split && st[kEvCount] <= (uint32_t)kEvCand) return;
+    EvictPiece x(a, e, seq_len, rowi, chunk);
+    if (x.S <= e.n_keep) {
+        int32_t* src = e.src ? e.src + (size_t)rowi * e.n_keep : nullptr;
+        if (src && !split)
+            for (int j = chunk * kEvChunk + tid; j < min(e.n_keep, (chunk + 1) * kEvChunk); j += kEvThreads) src[j] = j < x.S ? j : -1;
+        if (tid == 0 && chunk == 0) { e.moves[rowi] = -1; st[kEvCount] = 0; st[kEvDone] = 1; }
+        return;
+    }
+    if (chunk >= x.live()) return;
+    u32x4* const four = reinterpret_cast<u32x4*>(&sh.hist[4 * (kEvThreads - 1 - tid)]);
+    *four = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) evict_count(sh.hist, split ? x.k[u] >> 8 & 0xfffu : x.k[u] >> 20, x.j0 + u < x.S && (!split || x.k[u] >> 20 == prefix));
+    __syncthreads();
+    uint32_t* const g = c.hist + (size_t)rowi * kEvBins + 4 * (kEvThreads - 1 - tid);
+    const u32x4 h = *four;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (h[u]) atomicAdd(g + u, h[u]);
+    if (!evict_last(sh, c.arrived + rowi, x.live())) return;
+    u32x4 all;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) { all[u] = ldu_device(g + u); g[u] = 0u; }
+    evict_bin(sh, all, split ? st[kEvNeed] : (uint32_t)e.n_keep);
+    if (tid == 0) {
+        st[kEvKey] = split ? prefix << 12 | sh.bin[0] : sh.bin[0];
+        st[kEvNeed] = sh.bin[1];
+        st[kEvCount] = sh.bin[2];
+        st[kEvShift] = split ? 8u : 20u;
+        st[kEvDone] = 0u;
+    }
+}
+
+// grid (chunks, rows)
+template <typename T>
+__global__ __launch_bounds__(kEvThreads) void paged_evict_members_kernel(PagedCache a, EvictArgs e, EvictChain c, T* __restrict__ Kp, T* __restrict__ Vp,
+                                                                        int32_t* seq_len)
+{
+    __shared__ EvictShared sh;
+    __shared__ uint32_t sFree[kEvMaxChunks], sLate[kEvMaxChunks];
+    const int rowi = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
+    uint32_t* const st = c.state + (size_t)rowi * kEvState;
+    uint2* const cand = c.cand + (size_t)rowi * kEvCand;
+    uint2* const part = c.part + (size_t)rowi * c.chunks;
+    const uint32_t done = st[kEvDone], bin = st[kEvKey], shift = st[kEvShift], need0 = st[kEvNeed], members = st[kEvCount];
+    EvictPiece x(a, e, seq_len, rowi, chunk);
+    if (done || chunk >= x.live()) return;
+    const bool whole = need0 == members, few = members <= (uint32_t)kEvCand;   // the bin stays whole; its members can be ranked
+    if (!whole && !few) {
+        if (chunk == 0) {
+            evict_select<T, 0>(sh, a, e, Kp, Vp, seq_len, rowi);
+            if (tid == 0) st[kEvDone] = 1u;
+        }
+        return;
+    }
+    uint32_t frees = 0, lates = 0, opens = 0, mine = 0;   // of the wave; bit u: this lane's slot u is a member
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int j = x.j0 + u;
+        const uint32_t at = x.k[u] >> shift;
+        const bool in = j < x.S, open = in && at == bin && !whole, kept = in && (whole ? at >= bin : at > bin);
+        frees += (uint32_t)__popcll(__ballot(in && !open && !kept && j < e.n_keep));
+        lates += (uint32_t)__popcll(__ballot(kept && j >= e.n_keep));
+        opens += (uint32_t)__popcll(__ballot(open));
+        mine |= (uint32_t)open << u;
+    }
+    if (lane == 0) { sh.sumA[0][wave] = frees; sh.sumB[0][wave] = lates; sh.sumA[1][wave] = opens; }
+    __syncthreads();
+    uint32_t n_open;
+    uint32_t at_open = evict_before(sh.sumA[1], wave, &n_open);
+    if (tid == 0 && n_open) sh.last = atomicAdd(c.n_cand + rowi, n_open);   // the chunk's members take consecutive places
+    if (wave == 1) {
+        const uint32_t f = row16_sum_u32(sh.sumA[0][lane & 15]), l = row16_sum_u32(sh.sumB[0][lane & 15]);
+        if (lane == 0) stu2_device(part + chunk, f, l);
+    }
+    if (n_open) {   // uniform
+        __syncthreads();
+        const uint32_t n = (uint32_t)__popc(mine), incl = wave_incl_scan(n);
+        uint32_t to = sh.last + at_open + incl - n;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (mine >> u & 1) stu2_device(cand + to++, x.k[u], (uint32_t)(x.j0 + u));
+    }
+    const int n_chunks = x.live();
+    if (!evict_last(sh, c.arrived + rowi, n_chunks)) return;
+    if (tid == 0) c.n_cand[rowi] = 0u;
+    uint32_t f = 0, l = 0;
+    if (tid < n_chunks) {
+        const uint2 v = ldu2_device(part + tid);
+        f = v.x; l = v.y;
+    }
+    uint32_t key = (bin << shift) - 1u;   // the whole bin: what is above this
+    int slot = -1;
+    uint2 m[kEvCand / kEvThreads];
+    bool on[kEvCand / kEvThreads];
+#pragma unroll
+    for (int i = 0; i < kEvCand / kEvThreads; ++i) {
+        on[i] = !whole && (uint32_t)(tid + i * kEvThreads) < members;
+        m[i] = on[i] ? ldu2_device(cand + tid + i * kEvThreads) : make_uint2(0u, 0u);
+    }
+    if (!whole) {
+        uint32_t need = need0, n = members, prefix = bin, sft = shift;
+        bool settled = false;
+        for (int i = tid; i < kEvBins; i += kEvThreads) sh.hist[i] = 0;
+        if (tid == 0) sh.n_members = 0;
+        __syncthreads();
+        while (n > (uint32_t)kEvMembers && sft > 0) {   // the next 12 bits, the last 8
+            const uint32_t bits = min(12u, sft);
+            sft -= bits;
+#pragma unroll
+            for (int i = 0; i < kEvCand / kEvThreads; ++i)
+                evict_count(sh.hist, m[i].x >> sft & ((1u << bits) - 1), on[i] && m[i].x >> (sft + bits) == prefix);
+            __syncthreads();
+            u32x4* const four = reinterpret_cast<u32x4*>(&sh.hist[4 * (kEvThreads - 1 - tid)]);
+            const u32x4 h = *four;
+            *four = u32x4{0u, 0u, 0u, 0u};
+            evict_bin(sh, h, need);
+            prefix = prefix << bits | sh.bin[0];
+            need = sh.bin[1];
+            n = sh.bin[2];
+            if (need == n) { key = (prefix << sft) - 1u; slot = -1; settled = true; break; }
+            __syncthreads();   // (sh.bin is written again)
+        }
+        if (!settled && n <= (uint32_t)kEvMembers) {
+#pragma unroll
+            for (int i = 0; i < kEvCand / kEvThreads; ++i)
+                if (on[i] && m[i].x >> sft == prefix) {
+                    const uint32_t at = atomicAdd(&sh.n_members, 1u);
+                    sh.key[at] = m[i].x;
+                    sh.slot[at] = (int32_t)m[i].y;
+                }
+            __syncthreads();
+            evict_rank(sh, (int)n, need);
+            __syncthreads();
+            key = sh.bin[0];
+            slot = (int)sh.bin[1];
+        } else if (!settled) {   // one key, many slots, in no order: the need-th of them by halving
+            int lo = 0, hi = x.S - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                uint32_t below = 0;
+#pragma unroll
+                for (int i = 0; i < kEvCand / kEvThreads; ++i) below += (uint32_t)__popcll(__ballot(on[i] && m[i].x == prefix && (int)m[i].y <= mid));
+                __syncthreads();
+                if (lane == 0) sh.sumA[0][wave] = below;
+                __syncthreads();
+                if (wave_uniform((int)row16_sum_u32(sh.sumA[0][lane & 15])) >= (int)need) hi = mid;
+                else lo = mid + 1;
+            }
+            key = prefix;
+            slot = lo;
+        }
+    }
+    // the members' slots join what is certain
+    if (tid < kEvMaxChunks) { sFree[tid] = f; sLate[tid] = l; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEvCand / kEvThreads; ++i)
+        if (on[i]) {
+            const int j = (int)m[i].y;
+            const bool kept = m[i].x > key || (m[i].x == key && j <= slot);
+            if (!kept && j < e.n_keep) atomicAdd(&sFree[j / kEvChunk], 1u);
+            if (kept && j >= e.n_keep) atomicAdd(&sLate[j / kEvChunk], 1u);
+        }
+    __syncthreads();
+    f = tid < n_chunks ? sFree[tid] : 0u;
+    l = tid < n_chunks ? sLate[tid] : 0u;
+    const uint32_t fu = wave_incl_scan(f), lu = wave_incl_scan(l);
+    if (lane == kWave - 1) { sh.sumA[1][wave] = fu; sh.sumB[1][wave] = lu; }
+    __syncthreads();
+    uint32_t n_free, n_late;
+    const uint32_t f0 = evict_before(sh.sumA[1], wave, &n_free) + fu - f, l0 = evict_before(sh.sumB[1], wave, &n_late) + lu - l;
+    if (tid < n_chunks) part[tid] = make_uint2(f0, l0);
+    if (tid == 0) { st[kEvKey] = key; st[kEvSlot] = (uint32_t)slot; e.moves[rowi] = (int32_t)n_free; }
+}
+
+// grid (chunks, rows)
+__global__ __launch_bounds__(kEvThreads) void paged_evict_emit_kernel(PagedCache a, EvictArgs e, EvictChain c, const int32_t* __restrict__ seq_len)
+{
+    __shared__ uint32_t sums[kEvWaves];
+    const int rowi = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = wave_uniform(tid >> 6);
+    const uint32_t* const st = c.state + (size_t)rowi * kEvState;
+    const uint32_t done = st[kEvDone], key = st[kEvKey];
+    const int slot = (int)st[kEvSlot];
+    const uint2 place = c.part[(size_t)rowi * c.chunks + chunk];
+    EvictPiece x(a, e, seq_len, rowi, chunk);
+    if (done || chunk >= x.live()) return;
+    int32_t* src = e.src ? e.src + (size_t)rowi * e.n_keep : nullptr;
+    bool fr[4], lt[4];
+    uint32_t n = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int j = x.j0 + u;
+        const bool kept = j < x.S && (x.k[u] > key || (x.k[u] == key && j <= slot));
+        fr[u] = j < x.S && !kept && j < e.n_keep;
+        lt[u] = kept && j >= e.n_keep;
+        if (src && kept && j < e.n_keep) src[j] = j;
+        n += fr[u] ? 1u : lt[u] ? 0x10000u : 0u;   // (no more than 4096 of either)
+    }
+    const uint32_t incl = wave_incl_scan(n);
+    if (lane == kWave - 1) sums[wave] = incl;
+    __syncthreads();
+    uint32_t total;
+    const uint32_t before = evict_before(sums, wave, &total) + incl - n;
+    uint32_t f = place.x + (before & 0xffffu), l = place.y + (before >> 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (fr[u]) e.to[(size_t)rowi * e.move_cap + f++] = x.j0 + u;
+        if (lt[u]) e.from[(size_t)rowi * e.move_cap + l++] = x.j0 + u;
+    }
+}
+
 // grid (x, rows): the moves, `batch` of them a wave at a time; then the length
 template <typename T>
 __global__ __launch_bounds__(256) void paged_evict_move_kernel(PagedCache a, EvictArgs e, T* __restrict__ Kp, T* __restrict__ Vp, int32_t* seq_len, int batch)
@@ -1030,10 +1337,9 @@ __global__ __launch_bounds__(256) void paged_evict_move_kernel(PagedCache a, Evi
     for (int m = (blockIdx.x * 4 + wave) * batch; m < n; m += gridDim.x * 4 * batch) evict_move<T>(a, e, Kp, Vp, rowi, from + m, to + m, min(batch, n - m));
 }
 
-__global__ __launch_bounds__(256) void paged_clear_kernel(uint32_t* count, int n)
+__global__ __launch_bounds__(256) void paged_clear_kernel(uint32_t* words, size_t n)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) count[i] = 0u;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) words[i] = 0u;
 }
 
 }  // namespace sals

@@ -21,8 +21,9 @@ inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SA
 
 
 struct PagedLayout {  // byte offsets into the workspace
-    size_t count, sum, stat, final_stat, logits, moves, from, to, total;
-    int n_count, tiles, groups, rows, lds, move_cap, logit_stride;   // of the attention: head tiles, workgroups, query heads of one, LDS
+    size_t count, sum, stat, final_stat, logits, moves, from, to, hist, n_cand, arrived, state, cand, part, total;
+    size_t n_zero;   // words from `count` on that are zero between launches
+    int chunks, tiles, groups, rows, lds, move_cap, logit_stride;   // of the attention: head tiles, workgroups, query heads of one, LDS
 };
 
 inline int capacity(const sals_paged_desc& d) { return d.max_pages * d.page_size; }
@@ -52,7 +53,6 @@ PagedLayout make_layout(const sals_paged_desc& d)
     const size_t H = (size_t)d.B * d.H_q, cap = (size_t)capacity(d);
     const int group = d.H_q / d.H_kv, tiles = ceil_div(group, kPgHeads), single = d.H_kv * tiles, pairs = tiles == 1 && d.H_kv % 2 == 0 ? single / 2 : single;
     L.tiles = tiles;
-    L.n_count = d.B * single;
     // the kernel takes one KV head for each workgroup or two, by the lengths: room for either
     const int one = std::max(1, kPgGroups / single), two = std::max(1, kPgGroups / pairs);   // shares
     L.groups = std::max(one * single, two * pairs);
@@ -62,17 +62,32 @@ PagedLayout make_layout(const sals_paged_desc& d)
     L.move_cap = (int)cap / 2 + 1;   // (no more than half of the slots can move below the others)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes); return r; };
-    L.count = take((size_t)L.n_count * 4);
+    const size_t rows = (size_t)d.B * d.weight_heads;
+    // Eviction of long lists, a workgroup for each chunk of 4096 slots: beyond 32768 slots, and beyond 16384 as long as there are fewer lists
+    // than keep the compute units busy (32000 slots: 1 list 43 -> 28 us, 4 lists 49 -> 35, 64 lists 72 -> 74, 256 lists 191 -> 268;
+    // 16000 slots: 32 and 30, 37 and 36).
+    L.chunks = (int)cap > 8 * kEvChunk || ((int)cap > 4 * kEvChunk && rows < 64) ? ceil_div((int)cap, kEvChunk) : 0;
+    L.count = take((size_t)d.B * single * 4);
+    if (rows && L.chunks) {
+        L.n_cand = take(rows * 4);
+        L.arrived = take(rows * 4);
+        L.hist = take(rows * kEvBins * 4);
+    }
+    L.n_zero = at / 4;
     const size_t pieces = (size_t)2 * L.rows * std::max(one * single, 2 * two * pairs);
     L.sum = take(pieces * d.d * 4);
     L.stat = take(pieces * 8);
     L.final_stat = take(H * 8);
     if (d.weight_heads) {
-        const size_t rows = (size_t)d.B * d.weight_heads;
         L.logits = take(H * L.logit_stride * 4);
         L.moves = take(rows * 4);
         L.from = take(rows * L.move_cap * 4);
         L.to = take(rows * L.move_cap * 4);
+        if (L.chunks) {
+            L.state = take(rows * kEvState * 4);
+            L.cand = take(rows * kEvCand * 8);
+            L.part = take(rows * L.chunks * 8);
+        }
     }
     L.total = at;
     return L;
@@ -161,17 +176,28 @@ sals_status launch_evict(const sals_paged* c, const int32_t* q_pos, const int32_
     e.lists = d.weight_heads; e.n_keep = n_keep; e.n_sink = n_sink; e.n_recent = n_recent; e.move_cap = c->L.move_cap; e.D = d.d;
     const int rows = d.B * d.weight_heads, most = std::min(n_keep, a.cap - n_keep);   // moves of a list
     e.fused = most <= kEvFused;
-    auto select = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(rows), dim3(kEvThreads), 0, st, a, e, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len);
-    };
-    if (a.cap <= kEvChunk) select(paged_evict_select_kernel<T, 1>);
-    else if (a.cap <= 2 * kEvChunk) select(paged_evict_select_kernel<T, 2>);
-    else if (a.cap <= 8 * kEvChunk) select(paged_evict_select_kernel<T, 8>);
-    else select(paged_evict_select_kernel<T, 0>);
+    T *const K = static_cast<T*>(Kp), *const V = static_cast<T*>(Vp);
+    if (!c->L.chunks) {
+        if (a.cap <= kEvChunk) hipLaunchKernelGGL((paged_evict_select_kernel<T, 1>), dim3(rows), dim3(kEvThreads), 0, st, a, e, K, V, seq_len);
+        else if (a.cap > 2 * kEvChunk) hipLaunchKernelGGL((paged_evict_select_kernel<T, 8>), dim3(rows), dim3(kEvThreads), 0, st, a, e, K, V, seq_len);
+        else hipLaunchKernelGGL((paged_evict_select_kernel<T, 2>), dim3(rows), dim3(kEvThreads), 0, st, a, e, K, V, seq_len);
+    } else {
+        e.fused = 0;
+        const EvictChain ch{at<uint32_t>(c, c->L.hist), at<uint32_t>(c, c->L.n_cand), at<uint32_t>(c, c->L.arrived), at<uint32_t>(c, c->L.state),
+                            at<uint2>(c, c->L.cand), at<uint2>(c, c->L.part), c->L.chunks};
+        const dim3 grid(c->L.chunks, rows);
+        hipLaunchKernelGGL(paged_evict_hist_kernel, grid, dim3(kEvThreads), 0, st, a, e, ch, seq_len, 0);
+        if (launch_status() != SALS_OK) return SALS_ERR_HIP;
+        if (a.cap > (1 << 17)) hipLaunchKernelGGL(paged_evict_hist_kernel, grid, dim3(kEvThreads), 0, st, a, e, ch, seq_len, 1);
+        if (launch_status() != SALS_OK) return SALS_ERR_HIP;
+        hipLaunchKernelGGL((paged_evict_members_kernel<T>), grid, dim3(kEvThreads), 0, st, a, e, ch, K, V, seq_len);
+        if (launch_status() != SALS_OK) return SALS_ERR_HIP;
+        hipLaunchKernelGGL(paged_evict_emit_kernel, grid, dim3(kEvThreads), 0, st, a, e, ch, seq_len);
+    }
     if (launch_status() != SALS_OK || e.fused) return launch_status();
     // whole rows: eight moves a wave, a head's part of them: 16
     const int batch = e.lists == 1 && d.H_kv > 1 ? 8 : 16, x = std::max(1, std::min(ceil_div(4096, rows), ceil_div(most, 4 * batch)));
-    hipLaunchKernelGGL((paged_evict_move_kernel<T>), dim3(x, rows), dim3(256), 0, st, a, e, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len, batch);
+    hipLaunchKernelGGL((paged_evict_move_kernel<T>), dim3(x, rows), dim3(256), 0, st, a, e, K, V, seq_len, batch);
     return launch_status();
 }
 
@@ -220,7 +246,8 @@ sals_status sals_paged_prepare(sals_paged* ctx, void* hip_stream)
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(st, &cap) != hipSuccess) return SALS_ERR_HIP;
     if (cap != hipStreamCaptureStatusNone) return SALS_ERR_INVALID_ARG;
-    hipLaunchKernelGGL(paged_clear_kernel, dim3(ceil_div(ctx->L.n_count, 256)), dim3(256), 0, st, at<uint32_t>(ctx, ctx->L.count), ctx->L.n_count);
+    hipLaunchKernelGGL(paged_clear_kernel, dim3((unsigned)std::min<size_t>(4096, (ctx->L.n_zero + 255) / 256)), dim3(256), 0, st, at<uint32_t>(ctx, ctx->L.count),
+                       ctx->L.n_zero);
     if (launch_status() != SALS_OK || hipStreamSynchronize(st) != hipSuccess) return SALS_ERR_HIP;
 #define SALS_CALL(T, D) allow_attend_lds<T, D>(ctx)
     if (SALS_PAGED(ctx->d, SALS_CALL) != SALS_OK) return SALS_ERR_HIP;

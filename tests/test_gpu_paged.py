@@ -425,15 +425,15 @@ def test_evict(dtype, H_kv, d, P, per_head):
 
 
 @pytest.mark.parametrize("n,n_keep", [(4096, 4095), (4097, 1), (5000, 4096), (8192, 4097), (9001, 1003), (9001, 9000), (20000, 15000), (40000, 700), (40000, 39990),
-                                      (70000, 35000)])
+                                      (70000, 35000), (200000, 16384), (1048576, 500000)])
 def test_evict_long_lists(n, n_keep):
-    c = Cache([n, n - 1, n // 2], H=1, H_kv=1, d=64, P=64, lists=1)
+    c = Cache([n, n - 1, n // 2] if n < 1 << 20 else [n], H=1, H_kv=1, d=64, P=64, lists=1)
     _positions(c)
     _check_evict(c, n_keep, 4, min(64, n_keep // 2), src=n != 20000)
 
 
 @pytest.mark.parametrize("kind", ["equal", "zero", "ends", "nan", "two", "close", "negative"])
-@pytest.mark.parametrize("n,n_keep", [(300, 100), (5000, 4999), (6000, 2500)])
+@pytest.mark.parametrize("n,n_keep", [(300, 100), (5000, 4999), (6000, 2500), (9000, 8995), (20000, 9000), (140000, 70000)])
 def test_evict_weights_that_are_hard_to_rank(kind, n, n_keep):
     c = Cache([n, n - 7], H=2, H_kv=2, d=64, P=16, lists=2)
     _positions(c)
@@ -457,6 +457,17 @@ def test_evict_weights_that_are_hard_to_rank(kind, n, n_keep):
     else:
         w.copy_(r - 0.5)
     _check_evict(c, n_keep, 2, 10)
+
+
+def test_evict_the_same_context_again_and_shorter():
+    """Nothing of an eviction stays in the workspace: long lists, then short ones, then long ones again on one context."""
+    c = Cache([30000, 9000, 2000], H=2, H_kv=2, d=64, P=16, lists=2)
+    for lens, n_keep in (([30000, 9000, 2000], 1000), ([900, 1001, 5], 999), ([30000, 29999, 1001], 1000), ([30000, 30000, 30000], 29990), ([0, 1, 1], 1)):
+        c.lens = lens
+        c.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        _positions(c, seed=n_keep)
+        c.weights.copy_(torch.rand(c.weights.shape, generator=torch.Generator().manual_seed(n_keep)))
+        _check_evict(c, n_keep, 3, 20)
 
 
 def test_evict_more_protected_than_stay_and_extreme_positions():
