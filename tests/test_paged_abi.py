@@ -121,7 +121,7 @@ def test_binding_checks_what_it_is_given(sb):
     """Types, sizes, layout and device: host tensors never get past the binding."""
     torch = pytest.importorskip("torch")
     c = sb.Paged.__new__(sb.Paged)
-    c.desc, c._dtype, c._index, c._capacity, c._row, c._page_stride = _desc(sb), torch.bfloat16, -1, 1600, 1024, 16 * 1024
+    c.desc, c._dtype, c._index, c._capacity, c._row, c._page, c._page_stride = _desc(sb), torch.bfloat16, -1, 1600, 1024, (16, 8, 128), 16 * 1024
     good = torch.zeros(64, dtype=torch.int32)
     assert c._take("w", "x", good, torch.int32, 64) == good.data_ptr()
     wide = torch.zeros(64, 2, dtype=torch.int32)
