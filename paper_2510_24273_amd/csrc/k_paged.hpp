@@ -47,46 +47,51 @@ __device__ __forceinline__ int64_t paged_row(const PagedCache& a, int b, int j, 
 }
 
 // ---- append ---------------------------------------------------------------------------------------------------------------------
-// A workgroup takes kAppTok consecutive new tokens of a sequence, all heads: cos / sin of its tokens once into LDS, then 16-byte
-// pieces.  With one workgroup per sequence (n_tok <= kAppTok) it advances the length itself, behind its own reading of it.
-constexpr int kAppTok = 8;
+// A stream of 4 H_kv D elements a token.  A workgroup takes `tok` consecutive new tokens of a sequence, all heads: cos / sin of its
+// tokens once into LDS, then 16-byte pieces, each of K with its partners' piece (which another lane of the wave asks for as well).  The
+// last of a sequence's workgroups advances the length: by then all have read it.  It counts behind the pieces: 500 workgroups of 8 tokens
+// that counted first queued up at the one address (4001 tokens x 6: 60 us, behind 52, 32 tokens each 41).  The rows are stored
+// past the caches, which hold the partners' pieces instead: 41 -> 33 (4.8 TB/s, what a copy reaches).
+constexpr int kAppTok = 32;   // tokens of a workgroup at most; fewer as long as there are not three workgroups for each compute unit
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                            const int32_t* __restrict__ q_pos, T* __restrict__ Kp, T* __restrict__ Vp,
-                                                           int32_t* seq_len, const int32_t* __restrict__ n_new, int n_tok,
-                                                           int32_t* __restrict__ pos, float* __restrict__ weights, int lists,
-                                                           double log2_theta, int style)
+                                                           int32_t* seq_len, uint32_t* count, const int32_t* __restrict__ n_new, int n_tok, int tok,
+                                                           int32_t* __restrict__ pos, float* __restrict__ weights, int lists, double log2_theta,
+                                                           int style)
 {
     constexpr int VEC = elem<T>::vec, NP = D / 2, PIECES = D / VEC;
     __shared__ float2 sCS[kAppTok][NP];
     __shared__ int64_t sRow[kAppTok];
-    const int b = blockIdx.y, t0 = blockIdx.x * kAppTok, tid = threadIdx.x;
+    const int b = blockIdx.y, t0 = blockIdx.x * tok, tid = threadIdx.x;
     const int have = min(max(seq_len[b], 0), a.cap);
     const int want = n_new ? min(max(n_new[b], 0), n_tok) : n_tok;
     const int n = min(want, a.cap - have);          // tokens that fit
-    const int nt = min(kAppTok, n - t0);
+    const int nt = min(tok, n - t0);
     const int row = a.H_kv * D, qp = q_pos[b];
     for (int i = tid; i < nt * NP; i += 256) sCS[i / NP][i % NP] = rope_turn(qp + t0 + i / NP, rope_frequency<D>(i % NP, log2_theta));
     if (tid < nt) sRow[tid] = paged_row(a, b, have + t0 + tid, row);
     __syncthreads();
-    if (gridDim.x == 1 && tid == 0 && n > 0) seq_len[b] = have + n;
     for (int i = tid; i < nt * lists; i += 256) {
-        const size_t at = ((size_t)b * lists + i / nt) * a.cap + have + t0 + i % nt;
-        pos[at] = qp + t0 + i % nt;
+        const int list = idiv(i, nt), t = i - list * nt;
+        const size_t at = ((size_t)b * lists + list) * a.cap + have + t0 + t;
+        pos[at] = qp + t0 + t;
         weights[at] = 0.f;
     }
-    const int pieces = a.H_kv * PIECES;              // of a token
+    const int pieces = a.H_kv * PIECES;             // of a token
     for (int i = tid; i < nt * pieces; i += 256) {
-        const int t = i / pieces, pc = i - t * pieces;
+        const int t = idiv(i, pieces), pc = i - t * pieces;
         const int64_t at = sRow[t];
         if (at < 0) continue;
         const size_t from = ((size_t)b * n_tok + t0 + t) * row + (size_t)pc * VEC;
-        *reinterpret_cast<u32x4*>(Vp + at + (size_t)pc * VEC) = ld16(v_new + from);
-        // a piece of K and the piece of its partners: the same one for neighbouring pairs, half a head away otherwise
+        // a piece of K, the piece of its partners (itself where neighbours are pairs, half a head away otherwise), a piece of V
         const int ch = pc % PIECES * VEC;
+        const bool first = ch < NP;
+        const u32x4 kx = ld16(k_new + from), ky = style ? kx : ld16(k_new + (first ? from + NP : from - NP)), v = ld16(v_new + from);
         float x[VEC], y[VEC], r[VEC];
-        elem<T>::unpack(ld16(k_new + from), x);
+        elem<T>::unpack(kx, x);
+        elem<T>::unpack(ky, y);
         if (style) {
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {
@@ -95,8 +100,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
                 r[e + 1] = fmaf(x[e + 1], cs.x, x[e] * cs.y);
             }
         } else {
-            const bool first = ch < NP;
-            elem<T>::unpack(ld16(k_new + (first ? from + NP : from - NP)), y);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const float2 cs = sCS[t][(ch + e) % NP];
@@ -104,25 +107,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
             }
         }
         u32x4 w;
-        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)f32_to_bf16(r[2 * e]) | (uint32_t)f32_to_bf16(r[2 * e + 1]) << 16;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(r[e]);
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) w[e] = (uint32_t)f32_to_bf16(r[2 * e]) | (uint32_t)f32_to_bf16(r[2 * e + 1]) << 16;
+            else w[e] = __float_as_uint(r[e]);
         }
-        *reinterpret_cast<u32x4*>(Kp + at + (size_t)pc * VEC) = w;
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(Kp + at + (size_t)pc * VEC));
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(Vp + at + (size_t)pc * VEC));
     }
-}
-
-// the lengths behind an append of several workgroups per sequence
-__global__ __launch_bounds__(256) void paged_advance_kernel(int32_t* seq_len, const int32_t* __restrict__ n_new, int n_tok, int cap, int B)
-{
-    const int b = blockIdx.x * 256 + threadIdx.x;
-    if (b >= B) return;
-    const int have = min(max(seq_len[b], 0), cap), want = n_new ? min(max(n_new[b], 0), n_tok) : n_tok;
-    const int n = min(want, cap - have);
-    if (n > 0) seq_len[b] = have + n;
+    if (tid == 0 && (gridDim.x == 1 || arrive(count + b, gridDim.x) == gridDim.x - 1) && n > 0) seq_len[b] = have + n;
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------

@@ -124,13 +124,11 @@ sals_status launch_append(const sals_paged* c, const void* k_new, const void* v_
                           int32_t* seq_len, const int32_t* n_new, int n_tok, int32_t* pos, float* weights, hipStream_t st)
 {
     const sals_paged_desc& d = c->d;
-    const dim3 grid(ceil_div(n_tok, kAppTok), d.B);
+    const int tok = (int)std::min<int64_t>(kAppTok, ((int64_t)d.B * n_tok + 767) / 768);
+    const dim3 grid(ceil_div(n_tok, tok), d.B);
     hipLaunchKernelGGL((paged_append_kernel<T, D>), grid, dim3(256), 0, st, cache_of(c, table, seq_len), static_cast<const T*>(k_new),
-                       static_cast<const T*>(v_new), q_pos, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len, n_new, n_tok, pos, weights,
-                       d.weight_heads, c->log2_theta, d.rope_style);
-    if (launch_status() != SALS_OK) return SALS_ERR_HIP;
-    if (grid.x == 1) return SALS_OK;
-    hipLaunchKernelGGL(paged_advance_kernel, dim3(ceil_div(d.B, 256)), dim3(256), 0, st, seq_len, n_new, n_tok, capacity(d), d.B);
+                       static_cast<const T*>(v_new), q_pos, static_cast<T*>(Kp), static_cast<T*>(Vp), seq_len, at<uint32_t>(c, c->L.count), n_new, n_tok, tok,
+                       pos, weights, d.weight_heads, c->log2_theta, d.rope_style);
     return launch_status();
 }
 
