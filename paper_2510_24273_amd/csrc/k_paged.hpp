@@ -148,9 +148,11 @@ struct PagedWork {
     __device__ __forceinline__ int begin(int w) const { return w * q + min(w, r); }
     __device__ __forceinline__ int share(int x) const   // the one that block x belongs to
     {
-        const uint32_t split = (uint32_t)r * (uint32_t)(q + 1);
-        return (uint32_t)x < split ? (int)((uint32_t)x / (uint32_t)(q + 1)) : r + (int)(((uint32_t)x - split) / (uint32_t)q);
+        const int split = r * (q + 1);
+        return x < split ? per_share(x, q + 1) : r + per_share(x - split, q);
     }
+    // x / d; 24 bits divide in half the instructions
+    __device__ __forceinline__ int per_share(int x, int d) const { return blocks < 1 << 24 ? idiv(x, d) : (int)((uint32_t)x / (uint32_t)d); }
 };
 
 struct PagedParts {               // pieces of shared sequences: slot 2 w of share w for one that began before it, 2 w + 1 for one that goes on behind
@@ -248,7 +250,19 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     W.shares = min(max(1, idiv(kPgGroups, heads)), W.blocks);
     const int w = idiv(blockIdx.x, heads);
     if (w >= W.shares) return;
-    W.q = (int)((uint32_t)W.blocks / (uint32_t)W.shares);
+    // A sequence that begins in a share costs it the end of one stream and the start of another, as much as some blocks, which are dealt
+    // with the real ones (32 sequences of 188 to 6002 slots: 78.6 -> 74.4 us, with 4 to 16 of them alike); not where all are equally long and
+    // whole numbers of shares (8 x 8191 slots: 67.5, with them 68.4).
+    int pad = 0;
+    W.q = W.per_share(W.blocks, W.shares);
+    if (W.q >= 8) {
+        const bool even = per == 1 && wave_min_u32(lane0 < B ? mine : 0xffffffffu) == wave_max_u32(mine) && W.shares - idiv(W.shares, B) * B == 0;
+        if (!even) {
+            pad = min(4, W.q / 8);
+            W.blocks += pad * B;
+            W.q = W.per_share(W.blocks, W.shares);
+        }
+    }
     W.r = W.blocks - W.q * W.shares;
     // a workgroup's query heads are consecutive, nh for each of its KV heads
     const int hg = blockIdx.x - w * heads, sub = two ? wave >> 2 : 0, H = a.H_kv * a.group;
@@ -258,10 +272,10 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     const int wave_of = two ? wave & 3 : wave;   // of the KV head
     int at = W.begin(w);
     const int end = W.begin(w + 1);
-    const int first_lane = __popcll(__ballot(upto <= (uint32_t)at));
-    int b = first_lane * per, base = __builtin_amdgcn_readlane((int)(upto - mine), first_lane);
+    const int first_lane = __popcll(__ballot(upto + (uint32_t)(pad * min(B, (lane0 + 1) * per)) <= (uint32_t)at));
+    int b = first_lane * per, base = __builtin_amdgcn_readlane((int)(upto - mine), first_lane) + pad * b;
     auto length_of = [&](int s) { return per == 1 ? __builtin_amdgcn_readlane(lane_len, s) : wave_uniform(clamped(seq_len[s])); };
-    for (int n; base + (n = blocks_in(length_of(b))) <= at; ++b) base += n;
+    for (int n; base + (n = pad + blocks_in(length_of(b))) <= at; ++b) base += n;
 
     for (bool again = false; at < end; again = true) {
         if (again) __syncthreads();   // (LDS is taken anew)
@@ -269,8 +283,9 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         int tid = tid0;
         asm volatile("" : "+v"(tid));
         int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
-        const int S = length_of(b), n_blocks = blocks_in(S);
-        const int blk0 = at - base, blk1 = min(end - base, n_blocks), live1 = min(blk1, (S + TB - 1) / TB);
+        const int S = length_of(b), n_blocks = pad + blocks_in(S);
+        const bool begins = at == base;
+        const int blk0 = max(0, at - base - pad), blk1 = min(end - base, n_blocks) - pad, live1 = min(blk1, (S + TB - 1) / TB);
         const int32_t* tb = a.table + (size_t)b * a.max_pages;
 
         // ---- pages and rows of a block ----
@@ -351,6 +366,10 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             load_k(I0, blk);
             load_v(I0, blk);
         }
+
+        // the shares that this sequence is spread over
+        const bool ends = blk1 == n_blocks - pad, alone = begins && ends;
+        const int w0 = begins ? w : W.share(base), w1 = ends ? w : W.share(base + n_blocks - 1);
 
         // ---- the rotated query of these heads, scaled ----
         {
@@ -486,8 +505,6 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         asm volatile("" : "+v"(tid));
         lane = tid & 63; n16 = lane & 15; c4 = lane >> 4;
         const int n_live = min(WPH, live1 - blk0);        // waves of a KV head that had a block
-        const bool alone = blk0 == 0 && blk1 == n_blocks;
-        const int w0 = W.share(base), w1 = W.share(base + n_blocks - 1);   // the shares that this sequence is spread over
         if (wave_of < n_live) {
             l = sum_xor_rows(l);
             if (lane < kPgHeads) { sM[wave][lane] = m; sL[wave][lane] = l; }
@@ -513,7 +530,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             for (int e = 0; e < 4; ++e) elem<T>::store(to + e, y[e]);
             if (quad % (D / 4) == 0) parts.final_stat[h] = make_float2(L != 0.f ? Mh : 0.f, inv);
         };
-        const size_t piece = ((size_t)(2 * w + (blk0 == 0)) * heads + hg) * (HPW * parts.rows);
+        const size_t piece = ((size_t)(2 * w + begins) * heads + hg) * (HPW * parts.rows);
         for (int quad = tid; quad < quads; quad += THREADS) {
             const int hh = quad / (D / 4), s = two && hh >= nh ? 1 : 0, h = hh - s * nh;
             float mv[kPgWaves], lv[kPgWaves];
@@ -620,20 +637,43 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     }
 }
 
-// weights[b, list, j] += sum over the list's heads of the softmax weight.  grid (x, lists, B)
+// weights[b, list, j] += sum over the list's heads, in their order, of the softmax weight.  grid (x, lists, B); a thread takes four slots at a
+// time; its first logits are requested before the length and the statistics are there (the call's second launch: 8 x 8191 slots,
+// 32 heads: 5 us).
 __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const float* __restrict__ logits, const float2* __restrict__ stat,
                                                             int logit_stride, float* __restrict__ weights)
 {
-    const int lists = gridDim.y, b = blockIdx.z, H = a.H_kv * a.group, nh = H / lists, h0 = blockIdx.y * nh;
+    constexpr int AHEAD = 4;
+    __shared__ float2 sStat[1024];
+    const int lists = gridDim.y, b = blockIdx.z, H = a.H_kv * a.group, nh = idiv(H, lists), tid = threadIdx.x;
+    const size_t h0 = (size_t)b * H + blockIdx.y * nh;
+    const float* const x0 = logits + h0 * logit_stride;
+    float* const w = weights + ((size_t)b * lists + blockIdx.y) * a.cap;
+    int j = (blockIdx.x * 256 + tid) * 4;
+    f32x4 x[AHEAD];
+    auto request = [&](int h) {   // (rows of logits go on to a multiple of 32 slots)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) x[u] = *reinterpret_cast<const f32x4*>(x0 + (size_t)min(h + u, nh - 1) * logit_stride + j);
+    };
+    if (j < a.cap) request(0);
     const int S = min(max(a.seq_len[b], 0), a.cap);
-    float* w = weights + ((size_t)b * lists + blockIdx.y) * a.cap;
-    for (int j = blockIdx.x * 256 + threadIdx.x; j < S; j += gridDim.x * 256) {
-        float sum = 0.f;
-        for (int h = 0; h < nh; ++h) {
-            const float2 st = stat[(size_t)b * H + h0 + h];
-            sum += exp2f(logits[((size_t)b * H + h0 + h) * logit_stride + j] - st.x) * st.y;
+    for (int h = tid; h < nh; h += 256) sStat[h] = stat[h0 + h];
+    __syncthreads();
+    for (bool first = true; j < S; j += gridDim.x * 1024, first = false) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < nh; h += AHEAD) {
+            if (!first || h > 0) request(h);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (h + u < nh) {
+                    const float2 st = sStat[h + u];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(__builtin_amdgcn_exp2f(x[u][e] - st.x), st.y, sum[e]);
+                }
         }
-        w[j] += sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < S) w[j + e] += sum[e];
     }
 }
 

@@ -156,7 +156,7 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
                        static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits,
                        L.logit_stride, scale, c->log2_theta, d.rope_style);
     if (launch_status() != SALS_OK || !weights) return launch_status();
-    hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 256)), d.weight_heads, d.B), dim3(256), 0, st, a, logits,
+    hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 1024)), d.weight_heads, d.B), dim3(256), 0, st, a, logits,
                        at<float2>(c, L.final_stat), L.logit_stride, weights);
     return launch_status();
 }
