@@ -459,7 +459,7 @@ typedef struct {
     int32_t page_size;    /* rows of a page, 1 .. 2048                                      */
     int32_t max_pages;    /* entries of a sequence's table; max_pages * page_size <= 2^20   */
     int32_t n_pages;      /* pages of the pool                                              */
-    int32_t weight_heads; /* 0 | 1 | H_kv                                                   */
+    int32_t weight_heads; /* 0 | 1 | H_kv;  B * weight_heads <= 65535                       */
     int64_t page_stride;  /* elements from page to page: at least page_size * H_kv * d and a multiple of 16 bytes; 0: exactly that */
     float   rope_theta;   /* as in sals_desc                                                */
     int32_t rope_style;

@@ -40,6 +40,7 @@ sals_status validate(const sals_paged_desc* d)
     // what the kernels cover
     if (d->d != 64 && d->d != 128) return SALS_ERR_UNSUPPORTED;
     if (d->B > 1024 || d->H_q > 1024 || d->page_size > 2048) return SALS_ERR_UNSUPPORTED;
+    if ((int64_t)d->B * d->weight_heads > 65535) return SALS_ERR_UNSUPPORTED;
     if ((int64_t)d->max_pages * d->page_size > (1 << 20)) return SALS_ERR_UNSUPPORTED;
     const int64_t page = (int64_t)d->page_size * d->H_kv * d->d, vec = d->dtype == SALS_BF16 ? 8 : 4;
     if (d->page_stride != 0 && (d->page_stride < page || d->page_stride % vec != 0)) return SALS_ERR_INVALID_ARG;
@@ -138,8 +139,9 @@ template <typename T, int D> auto attend_kernel(const sals_paged* c)
 }
 template <typename T, int D> sals_status allow_attend_lds(const sals_paged* c)
 {
+    // (of the kernel, not of the context: what the largest group takes)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c)), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               c->L.lds) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
+                               kPgWaves * kPgHeads * (D + 4) * 4) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
 }
 
 template <typename T, int D>

@@ -138,7 +138,8 @@ def test_lengths_from_none_to_long(dtype, d):
     c.check_attend(before)
 
 
-@pytest.mark.parametrize("H,H_kv", [(1, 1), (4, 4), (8, 2), (8, 1), (32, 8), (12, 4), (20, 1), (15, 5), (64, 8), (40, 2), (34, 2), (96, 32)])
+@pytest.mark.parametrize("H,H_kv", [(1, 1), (4, 4), (8, 2), (8, 1), (32, 8), (12, 4), (20, 1), (15, 5), (64, 8), (40, 2), (34, 2), (96, 32),
+                                    (300, 300), (512, 256), (1024, 1)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_head_layouts(H, H_kv, dtype):
     for lists in ((1, H_kv) if H_kv > 1 else (1,)):
@@ -283,6 +284,31 @@ def test_results_repeat_bit_for_bit_and_without_weights_too():
         assert torch.equal(o.view(torch.int16), runs[0][0].view(torch.int16)) and torch.equal(w, runs[0][1])
     assert torch.equal(c.out.view(torch.int16), runs[0][0].view(torch.int16))
     assert torch.equal(c.weights, runs[0][1])
+
+
+def test_contexts_of_different_groups_side_by_side():
+    """What one context needs of a kernel is not taken away by another one's set-up."""
+    big, small = Cache([300, 40], H=32, H_kv=2, P=16), Cache([300, 40], H=2, H_kv=2, P=16, seed=1)
+    for c in (big, small, big):
+        c.out.fill_(float("nan"))
+        c.attend()
+        torch.cuda.synchronize()
+        c.check_attend()
+
+
+def test_one_context_for_two_caches_and_changing_lengths():
+    """Nothing of a call stays in the workspace: other caches, lengths, one KV head or two in a workgroup, on one context."""
+    c = Cache([9000, 8000, 3], H=16, H_kv=8, P=16, lists=8)
+    full = [t.clone() for t in (c.Kp, c.Vp)]
+    for lens in ([9000, 8000, 3], [1, 0, 0], [700, 33, 3], [9000, 8000, 0], [5, 8000, 1]):
+        c.lens = lens
+        c.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        before = c.weights.clone()
+        c.attend()
+        torch.cuda.synchronize()
+        c.check_attend(before)
+        c.Kp, c.Vp = c.Vp, c.Kp
+    assert torch.equal(c.Vp.view(torch.int16), full[0].view(torch.int16)) and torch.equal(c.Kp.view(torch.int16), full[1].view(torch.int16))
 
 
 def test_offsets_past_32_bits():

@@ -30,7 +30,7 @@ def _desc(sb, **kw):
     (dict(weight_heads=2), 1), (dict(weight_heads=-1), 1), (dict(rope_theta=0.0), 1), (dict(rope_theta=float("inf")), 1), (dict(rope_style=2), 1),
     (dict(page_stride=16 * 8 * 128 - 8), 1), (dict(page_stride=16 * 8 * 128 + 4), 1), (dict(page_stride=-8), 1), (dict(d=3), 1),
     (dict(d=96), 2), (dict(d=256), 2), (dict(B=1025), 2), (dict(H_q=2048), 2), (dict(page_size=2049), 2), (dict(max_pages=65537), 2),
-    (dict(page_stride=1 << 50), 2)])
+    (dict(B=1024, H_q=64, H_kv=64, weight_heads=64), 2), (dict(page_stride=1 << 50), 2)])
 def test_descriptors_that_are_refused(sb, kw, code):
     with pytest.raises(sb.SalsError) as e:
         sb.paged_workspace_bytes(_desc(sb, **kw))
