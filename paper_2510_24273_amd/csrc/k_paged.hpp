@@ -22,8 +22,8 @@ struct PagedCache {           // the cache of one layer and the shape of the cal
     int32_t B, H_kv, group;   // group: query heads of a KV head
 };
 
-// cos / sin of position * theta^(-2 pair / D): the angle in turns, in fp64, less its whole part; what is left is exact to 1e-16 * position
-// turns and goes to fp32 (half a step of a value of at most 1/2 turn: 9e-8 radians).
+// cos / sin of position * theta^(-2 pair / D): the angle in turns, in fp64, less its whole part (what is left is exact to
+// 1e-16 * position turns); cos and sin of its fp32 value, and one step of their series for what that leaves out.
 template <int D> __device__ __forceinline__ double rope_frequency(int pair, double log2_theta)   // turns per position
 {
     return exp2(-(double)pair * (2.0 / D) * log2_theta) * kInvTwoPi;
@@ -31,12 +31,12 @@ template <int D> __device__ __forceinline__ double rope_frequency(int pair, doub
 __device__ __forceinline__ float2 rope_turn(int position, double frequency)
 {
     const double t = (double)position * frequency;
+    const double part = t - rint(t);
+    const float f = (float)part, rest = (float)((part - (double)f) * (1.0 / kInvTwoPi));
     float s, c;
-    sincospif(2.f * (float)(t - rint(t)), &s, &c);
-    return make_float2(c, s);
+    sincospif(2.f * f, &s, &c);
+    return make_float2(fmaf(-rest, s, c), fmaf(rest, c, s));
 }
-template <int D> __device__ __forceinline__ int pair_lo(int p, int style) { return style ? 2 * p : p; }
-template <int D> __device__ __forceinline__ int pair_hi(int p, int style) { return style ? 2 * p + 1 : p + D / 2; }
 
 // element offset of slot j's row, or -1 where its page is not there
 __device__ __forceinline__ int64_t paged_row(const PagedCache& a, int b, int j, int row)
@@ -401,9 +401,10 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         for (; blk < live1; blk += WPH) {
             const int t0 = blk * TB;
             const bool more = blk + WPH < live1;
-            f32x4 x[NKT];
+            constexpr int CHAINS = BF ? 1 : 4;   // fp32: sums of a quarter of the channels each, whose roundings add up less
+            f32x4 x[NKT > CHAINS ? NKT : CHAINS];
 #pragma unroll
-            for (int t = 0; t < NKT; ++t) x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < (BF ? NKT : CHAINS); ++t) x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
             int at_lane = lane;
             asm volatile("" : "+v"(at_lane));   // (read from LDS for every block: the registers are wanted for rows)
 #pragma unroll
@@ -418,10 +419,11 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(K[t][s][e]), __uint_as_float(qv[e]), x[t], 0, 0, 0);
+                                x[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(K[t][s][e]), __uint_as_float(qv[e]), x[e], 0, 0, 0);
                         }
                     }
                 }
+            if constexpr (!BF) x[0] = (x[0] + x[1]) + (x[2] + x[3]);
             // which of this lane's slots count (slot t0 + CH c4 + e is x[e / 4][e % 4])
             bool whole = t0 + TB <= S;
 #pragma unroll
