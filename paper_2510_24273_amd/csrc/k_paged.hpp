@@ -241,14 +241,24 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     const uint32_t upto = wave_incl_scan(mine);
     PagedWork W;
     W.blocks = __builtin_amdgcn_readlane((int)upto, 63);
-    // Two neighbouring KV heads of a workgroup, four waves for each, read twice as long pieces of memory, and the channels that are slow
-    // for every fourth 256 bytes are shared out; a sequence then has twice as many pieces to join.  From 16 blocks for each workgroup
-    // on that is worth it (32 heads, 16 x 4096 slots: 177 -> 167 us; 8 heads, 8 x 8191: 62 -> 60; 8 heads, 4100 slots: 13.7 -> 18.7).
-    const int single = kv_heads * tiles;
-    const bool two = tiles == 1 && !(kv_heads & 1) && W.blocks >= idiv(16 * kPgGroups, single);
-    const int HPW = two ? 2 : 1, WPH = two ? kPgWaves / 2 : kPgWaves, heads = two ? single >> 1 : single;
+    // Two neighbouring KV heads of a workgroup, four waves for each, read longer pieces of memory, and the channels that are slow for every
+    // fourth 256 bytes are shared out; a sequence then has twice as many pieces to join.  Worth it from 16 blocks for each workgroup on,
+    // where a sequence has no more than about 16 pieces or is long (32 heads, 16 x 4096 slots: 177 -> 167 us; 8 heads, 8 x 8191: 62 -> 60;
+    // 1 x 4100: 13.7, with two 18.7; 1 x 32768: 30, with two 34).  Four with two waves each: 172, and no faster for heads of 64 channels.
+    const int single = kv_heads * tiles, per_group = idiv(kPgGroups, single);
+    const int lg = tiles == 1 && !(kv_heads & 1) && W.blocks >= 16 * per_group && (2 * per_group <= 16 * B || W.blocks >= 128 * per_group) ? 1 : 0;
+    const int HPW = 1 << lg, WPH = kPgWaves >> lg, heads = single >> lg;
     W.shares = min(max(1, idiv(kPgGroups, heads)), W.blocks);
-    const int w = idiv(blockIdx.x, heads);
+    // Workgroup -> share and KV heads.  Tiles of 16 query heads that read the same rows lie 8 apart, on one die and its L2.
+    int w, hg;
+    if (tiles == 1) {
+        w = idiv(blockIdx.x, heads);
+        hg = blockIdx.x - w * heads;
+    } else {
+        const int eight = idiv(blockIdx.x >> 3, tiles), c = eight * 8 + (blockIdx.x & 7);
+        w = idiv(c, kv_heads);
+        hg = (c - w * kv_heads) * tiles + (blockIdx.x >> 3) - eight * tiles;
+    }
     if (w >= W.shares) return;
     // A sequence that begins in a share costs it the end of one stream and the start of another, as much as some blocks, which are dealt
     // with the real ones (32 sequences of 188 to 6002 slots: 78.6 -> 74.4 us, with 4 to 16 of them alike); not where all are equally long and
@@ -265,11 +275,11 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     }
     W.r = W.blocks - W.q * W.shares;
     // a workgroup's query heads are consecutive, nh for each of its KV heads
-    const int hg = blockIdx.x - w * heads, sub = two ? wave >> 2 : 0, H = a.H_kv * a.group;
-    const int g = two ? 2 * hg + sub : tiles == 1 ? hg : idiv(hg, tiles);
+    const int sub = wave >> (3 - lg), H = a.H_kv * a.group;
+    const int g = tiles == 1 ? hg * HPW + sub : idiv(hg, tiles);
     const int first_head = tiles == 1 ? hg * HPW * a.group : g * a.group + (hg - g * tiles) * kPgHeads;
     const int nh = min(kPgHeads, (g + 1) * a.group - first_head - sub * a.group), h0 = first_head + sub * a.group;
-    const int wave_of = two ? wave & 3 : wave;   // of the KV head
+    const int wave_of = wave & (WPH - 1);   // of the KV head
     int at = W.begin(w);
     const int end = W.begin(w + 1);
     const int first_lane = __popcll(__ballot(upto + (uint32_t)(pad * min(B, (lane0 + 1) * per)) <= (uint32_t)at));
@@ -534,7 +544,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         };
         const size_t piece = ((size_t)(2 * w + begins) * heads + hg) * (HPW * parts.rows);
         for (int quad = tid; quad < quads; quad += THREADS) {
-            const int hh = quad / (D / 4), s = two && hh >= nh ? 1 : 0, h = hh - s * nh;
+            const int hh = quad / (D / 4), s = hh >= nh ? 1 : 0, h = hh - s * nh;
             float mv[kPgWaves], lv[kPgWaves];
             f32x4 ov[kPgWaves];
 #pragma unroll

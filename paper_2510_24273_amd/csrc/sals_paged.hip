@@ -52,13 +52,18 @@ PagedLayout make_layout(const sals_paged_desc& d)
 {
     PagedLayout L{};
     const size_t H = (size_t)d.B * d.H_q, cap = (size_t)capacity(d);
-    const int group = d.H_q / d.H_kv, tiles = ceil_div(group, kPgHeads), single = d.H_kv * tiles, pairs = tiles == 1 && d.H_kv % 2 == 0 ? single / 2 : single;
+    const int group = d.H_q / d.H_kv, tiles = ceil_div(group, kPgHeads), single = d.H_kv * tiles;
     L.tiles = tiles;
     // the kernel takes one KV head for each workgroup or two, by the lengths: room for either
-    const int one = std::max(1, kPgGroups / single), two = std::max(1, kPgGroups / pairs);   // shares
-    L.groups = std::max(one * single, two * pairs);
+    int pieces = 0, factors = 0;   // of query heads
+    for (int lg = 0; lg <= (tiles == 1 && d.H_kv % 2 == 0 ? 1 : 0); ++lg) {
+        const int heads = single >> lg, shares = std::max(1, kPgGroups / heads);
+        L.groups = std::max(L.groups, tiles > 1 ? ceil_div(shares * d.H_kv, 8) * 8 * tiles : shares * heads);
+        pieces = std::max(pieces, (2 * shares * heads) << lg);
+        factors = std::max(factors, shares << lg);
+    }
     L.rows = std::min(group, kPgHeads);
-    L.lds = 4 * std::max(kPgWaves * L.rows * (d.d + 4), L.rows * std::max(one, 2 * two));   // the waves' sums, or the factors of the pieces: up to 68 KB
+    L.lds = 4 * L.rows * std::max(kPgWaves * (d.d + 4), factors);   // the waves' sums, or the factors of the pieces: up to 66 KB
     L.logit_stride = ceil_div((int)cap, 32) * 32;
     L.move_cap = (int)cap / 2 + 1;   // (no more than half of the slots can move below the others)
     size_t at = 0;
@@ -75,9 +80,8 @@ PagedLayout make_layout(const sals_paged_desc& d)
         L.hist = take(rows * kEvBins * 4);
     }
     L.n_zero = at / 4;
-    const size_t pieces = (size_t)2 * L.rows * std::max(one * single, 2 * two * pairs);
-    L.sum = take(pieces * d.d * 4);
-    L.stat = take(pieces * 8);
+    L.sum = take((size_t)pieces * L.rows * d.d * 4);
+    L.stat = take((size_t)pieces * L.rows * 8);
     L.final_stat = take(H * 8);
     if (d.weight_heads) {
         L.logits = take(H * L.logit_stride * 4);
@@ -141,7 +145,7 @@ template <typename T, int D> sals_status allow_attend_lds(const sals_paged* c)
 {
     // (of the kernel, not of the context: what the largest group takes)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c)), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               kPgWaves * kPgHeads * (D + 4) * 4) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
+                               kPgHeads * std::max(kPgWaves * (D + 4), 2 * kPgGroups) * 4) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
 }
 
 template <typename T, int D>
