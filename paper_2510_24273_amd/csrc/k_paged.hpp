@@ -5,6 +5,8 @@
 #pragma once
 #include "common.hpp"
 
+#include <type_traits>
+
 namespace sals {
 
 constexpr double kInvTwoPi = 0.15915494309189533576888376337251;
@@ -191,6 +193,14 @@ __device__ __forceinline__ void st2_device(float2* p, float2 v)
 }
 __device__ __forceinline__ void device_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// a barrier for what was written to LDS; loads on their way stay there
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ float max_xor_rows(float v)   // over the four lanes that hold a head
 {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -353,28 +363,32 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             }
         };
 
-        // the query and its position come ahead of the first rows, which wait for the table: it is rotated while they are on their way
+        // the query and its position come with the table's entries, which the first rows wait for: it is rotated while those are on their way
         int blk = blk0 + wave_of;
+        // a thread's pair of channels in some of the 16 columns of every KV head (columns without a query head are zero)
+        constexpr int COLS = THREADS / (D / 2), NQ = 2 * kPgHeads / COLS;
+        const int pair = tid % (D / 2), ch1 = style ? 2 * pair : pair, ch2 = style ? 2 * pair + 1 : pair + D / 2;
+        const int position_v = ld_uniform_i32(q_pos + b);
+        typedef typename std::conditional<BF, uint16_t, uint32_t>::type Raw;
+        uint32_t q1[NQ], q2[NQ];   // bits; not set to anything first: behind a branch a value that is one of two would be waited for there
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            asm volatile("" : "=v"(q1[k]), "=v"(q2[k]));
+            const int col = tid / (D / 2) + k * COLS, h = col % kPgHeads;
+            if (h < nh && col < HPW * kPgHeads) {
+                const Raw* p = reinterpret_cast<const Raw*>(q) + ((size_t)b * H + first_head + col / kPgHeads * nh + h) * D;
+                q1[k] = p[ch1];
+                q2[k] = p[ch2];
+            }
+        }
         Ids I0, I1;
         if (blk < live1) {
             load_ids(I0, blk);
             load_ids(I1, blk + WPH);
         }
-        // a thread's pair of channels in some of the 16 columns of every KV head (columns without a query head are zero)
-        constexpr int COLS = THREADS / (D / 2), NQ = 2 * kPgHeads / COLS;
-        const int pair = tid % (D / 2), ch1 = style ? 2 * pair : pair, ch2 = style ? 2 * pair + 1 : pair + D / 2;
-        const int position_v = ld_uniform_i32(q_pos + b);
-        T q1[NQ], q2[NQ];
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) {
-            const int col = tid / (D / 2) + k * COLS, h = col % kPgHeads;
-            q1[k] = q2[k] = T(0);
-            if (h < nh && col < HPW * kPgHeads) {
-                const T* p = q + ((size_t)b * H + first_head + col / kPgHeads * nh + h) * D;
-                q1[k] = p[ch1];
-                q2[k] = p[ch2];
-            }
-        }
+        // (vmcnt(0), the other counters left alone: all of these are one trip to memory, and behind it the compiler knows that the query is
+        // there; it would wait for the rows with it otherwise)
+        __builtin_amdgcn_s_waitcnt(0x0f70);
         if (blk < live1) {
             load_k(I0, blk);
             load_v(I0, blk);
@@ -391,7 +405,8 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             for (int k = 0; k < NQ; ++k) {
                 const int col = tid / (D / 2) + k * COLS;
                 if (col >= HPW * kPgHeads) break;
-                const float x = elem<T>::load(&q1[k]), y = elem<T>::load(&q2[k]);
+                const bool live = col % kPgHeads < nh;
+                const float x = live ? __uint_as_float(q1[k] << (BF ? 16 : 0)) : 0.f, y = live ? __uint_as_float(q2[k] << (BF ? 16 : 0)) : 0.f;
                 float r[2] = {fmaf(x, cs.x, -(y * cs.y)) * scale, fmaf(y, cs.x, x * cs.y) * scale};
                 const int ch[2] = {ch1, ch2};
 #pragma unroll
@@ -404,16 +419,17 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                     }
             }
         }
-        __syncthreads();
+        lds_barrier();
 
         // ---- the stream ----
         float m = -INFINITY, l = 0.f;
         f32x4 O[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (; blk < live1; blk += WPH) {
+        // MORE: the block behind is requested.  (No branch around its loads: the compiler would wait for all that are under way, not
+        // knowing which ones are.)
+        auto block = [&](auto MORE) {
             const int t0 = blk * TB;
-            const bool more = blk + WPH < live1;
             constexpr int CHAINS = BF ? 1 : 4;   // fp32: sums of a quarter of the channels each, whose roundings add up less
             f32x4 x[NKT > CHAINS ? NKT : CHAINS];
 #pragma unroll
@@ -451,14 +467,9 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             const uint64_t part_of = __ballot(!whole);
             Ids I2;
             __builtin_amdgcn_sched_barrier(0);
-            if (more) {
+            if constexpr (MORE()) {
                 load_ids(I2, blk + 2 * WPH);
                 load_k(I1, blk + WPH);
-            }
-            if (logits && n16 < nh) {
-                float* to = logits + (size_t)((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
-#pragma unroll
-                for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = x[t];
             }
             float top = x[0][0];
 #pragma unroll
@@ -511,10 +522,19 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                     for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(V[e][j]), p[e], O[j], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);   // (the rows behind take these registers, not others)
-            if (more) load_v(I1, blk + WPH);
-            I0 = I1;
-            I1 = I2;
-        }
+            if constexpr (MORE()) {
+                load_v(I1, blk + WPH);
+                I0 = I1;
+                I1 = I2;
+            }
+            if (logits && n16 < nh) {
+                float* to = logits + (size_t)((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
+#pragma unroll
+                for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = x[t];
+            }
+        };
+        for (; blk + WPH < live1; blk += WPH) block(std::true_type{});
+        if (blk < live1) block(std::false_type{});
 
         // ---- the waves joined ----
         asm volatile("" : "+v"(tid));
