@@ -140,6 +140,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
 constexpr int kPgHeads = 16;           // query heads of a workgroup
 constexpr int kPgWaves = 8;
 constexpr int kPgGroups = 256;         // workgroups: one per compute unit
+constexpr int kPgKept = 2048;          // floats of logits that a wave keeps
 constexpr int kPgAhead = 8;            // pieces of a shared sequence that a thread requests together
 
 template <typename T> struct PgBlock;
@@ -212,13 +213,14 @@ __device__ __forceinline__ float sum_xor_rows(float v)
     return v + __shfl_xor(v, 32);
 }
 
-// grid: a workgroup for each compute unit (see `lg` for which work it gets); logits: null, or [B * H][logit_stride] to be left
+// grid: a workgroup for each compute unit (see `lg` for which work it gets); logits: null, or [B * H][logit_stride] to be left,
+// keep: the LDS for runs of them is there
 template <typename T, int D, bool WHOLE>   // WHOLE: the CH slots of a lane lie in one page
 __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const int32_t* __restrict__ seq_len, int B, int cap, int kv_heads, int tiles,
                                                                        PagedCache a, const T* __restrict__ q, const int32_t* __restrict__ q_pos,
                                                                        const T* __restrict__ Kp, const T* __restrict__ Vp, T* __restrict__ out,
-                                                                       PagedParts parts, float* __restrict__ logits, int logit_stride, float scale,
-                                                                       double log2_theta, int style)
+                                                                       PagedParts parts, float* __restrict__ logits, int logit_stride, int keep,
+                                                                       float scale, double log2_theta, int style)
 {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int TB = PgBlock<T>::TB, CH = TB / 4, VEC = elem<T>::vec;
@@ -426,6 +428,21 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
         f32x4 O[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) O[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // Logits that are wanted are kept in LDS and leave in runs, where a wave has more than two blocks: a few bytes stored beside every
+        // block slow the stream down (with the weights' launch, 16 x 4096 slots of 32 heads 201 -> 189 us, 8 x 8191 of 8 64 -> 61).
+        float* const kept = sO + wave * kPgKept;
+        const int keep_most = keep && live1 - blk0 > 2 * WPH ? idiv(kPgKept / TB, nh) : 0;
+        int n_kept = 0;   // blocks, `blk` the last one
+        auto leave = [&]() {
+            constexpr int PL = TB / 4;
+            const int first = blk - (n_kept - 1) * WPH;
+            for (int i = lane; i < n_kept * nh * PL; i += kWave) {
+                const int line = i / PL, k = idiv(line, nh), h = line - k * nh;
+                const f32x4 v = *reinterpret_cast<const f32x4*>(kept + i * 4);
+                *reinterpret_cast<f32x4*>(logits + ((size_t)b * H + h0 + h) * logit_stride + (size_t)(first + k * WPH) * TB + i % PL * 4) = v;
+            }
+            n_kept = 0;
+        };
         // MORE: the block behind is requested.  (No branch around its loads: the compiler would wait for all that are under way, not
         // knowing which ones are.)
         auto block = [&](auto MORE) {
@@ -527,14 +544,23 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                 I0 = I1;
                 I1 = I2;
             }
-            if (logits && n16 < nh) {
-                float* to = logits + (size_t)((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
+            if (keep_most > 0) {
+                if (n16 < nh)
+#pragma unroll
+                    for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(kept + (n_kept * nh + n16) * TB + c4 * CH + 4 * t) = x[t];
+                if (++n_kept == keep_most) leave();
+            } else if (logits && n16 < nh) {
+                float* to = logits + ((size_t)b * H + h0 + n16) * logit_stride + t0 + c4 * CH;
 #pragma unroll
                 for (int t = 0; t < NKT; ++t) *reinterpret_cast<f32x4*>(to + 4 * t) = x[t];
             }
         };
         for (; blk + WPH < live1; blk += WPH) block(std::true_type{});
         if (blk < live1) block(std::false_type{});
+        if (keep_most > 0) {   // (what is kept lies where the waves' sums come next)
+            leave();
+            lds_barrier();
+        }
 
         // ---- the waves joined ----
         asm volatile("" : "+v"(tid));

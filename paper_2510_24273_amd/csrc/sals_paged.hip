@@ -143,9 +143,9 @@ template <typename T, int D> auto attend_kernel(const sals_paged* c)
 }
 template <typename T, int D> sals_status allow_attend_lds(const sals_paged* c)
 {
-    // (of the kernel, not of the context: what the largest group takes)
+    // (of the kernel, not of the context: what the largest group takes, or logits that are kept)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(attend_kernel<T, D>(c)), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               kPgHeads * std::max(kPgWaves * (D + 4), 2 * kPgGroups) * 4) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
+                               std::max(kPgHeads * std::max(kPgWaves * (D + 4), 2 * kPgGroups), kPgWaves * kPgKept) * 4) == hipSuccess ? SALS_OK : SALS_ERR_HIP;
 }
 
 template <typename T, int D>
@@ -158,9 +158,11 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
     float* logits = weights ? at<float>(c, L.logits) : nullptr;
     const PagedParts parts{at<float>(c, L.sum), at<float2>(c, L.stat), at<uint32_t>(c, L.count), at<float2>(c, L.final_stat), L.rows};
     const float scale = (float)(1.4426950408889634074 / std::sqrt((double)D));
-    hipLaunchKernelGGL((attend_kernel<T, D>(c)), dim3(L.groups), dim3(kPgWaves * 64), L.lds, st, seq_len, d.B, a.cap, d.H_kv, L.tiles, a,
+    // (64 KB of LDS for runs of logits: not where no wave can have more than two blocks, 0.5 us)
+    const int keep = logits && (int64_t)d.B * ceil_div(a.cap, PgBlock<T>::TB) >= 16 * (kPgGroups / (d.H_kv * L.tiles)) ? 1 : 0;
+    hipLaunchKernelGGL((attend_kernel<T, D>(c)), dim3(L.groups), dim3(kPgWaves * 64), keep ? std::max(L.lds, kPgWaves * kPgKept * 4) : L.lds, st, seq_len, d.B, a.cap, d.H_kv, L.tiles, a,
                        static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits,
-                       L.logit_stride, scale, c->log2_theta, d.rope_style);
+                       L.logit_stride, keep, scale, c->log2_theta, d.rope_style);
     if (launch_status() != SALS_OK || !weights) return launch_status();
     hipLaunchKernelGGL(paged_weights_kernel, dim3(std::min(64, ceil_div(a.cap, 1024)), d.weight_heads, d.B), dim3(256), 0, st, a, logits,
                        at<float2>(c, L.final_stat), L.logit_stride, weights);
