@@ -446,6 +446,8 @@ class Paged:
     def append(self, k_new, v_new, q_pos, table, Kp, Vp, seq_len, n_tok=1, n_new=None, pos=None, weights=None):
         """n_tok new tokens per sequence (k_new, v_new [B, n_tok, H_kv, d]; n_new [B] int32 of them count) from position q_pos on."""
         w = "sals_paged_append"
+        if not 0 < n_tok < 1 << 31:
+            raise SalsError(SALS_ERR_INVALID_ARG, f"{w}: n_tok must be a count below 2^31")
         qp, tb, kp, vp, sl = self._common(w, q_pos, table, Kp, Vp, seq_len)
         n = self.desc.B * int(n_tok) * self._row
         self._check(_lib.sals_paged_append(
@@ -464,6 +466,8 @@ class Paged:
     def evict(self, q_pos, table, Kp, Vp, seq_len, pos, weights, n_keep, n_sink=0, n_recent=0, src=None):
         """Sequences longer than n_keep keep n_keep slots of every list; src [B, weight_heads, n_keep] int32: where each came from."""
         w = "sals_paged_evict"
+        if not all(0 <= n < 1 << 31 for n in (n_keep, n_sink, n_recent)):   # (larger ones would lose their upper bits on the way)
+            raise SalsError(SALS_ERR_INVALID_ARG, f"{w}: n_keep, n_sink and n_recent must be counts below 2^31")
         qp, tb, kp, vp, sl = self._common(w, q_pos, table, Kp, Vp, seq_len)
         self._check(_lib.sals_paged_evict(
             self._h, qp, tb, kp, vp, sl, self._lists(w, "pos", pos, torch.int32), self._lists(w, "weights", weights, torch.float32),

@@ -698,8 +698,8 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     }
 }
 
-// weights[b, list, j] += sum over the list's heads, in their order, of the softmax weight.  grid (x, lists, B); a thread takes four slots at a
-// time; its first logits are requested before the length and the statistics are there (the call's second launch: 8 x 8191 slots,
+// weights[b, list, j] += sum over the list's heads, in their order, of the softmax weight.  grid (x, lists, B); a thread takes four slots
+// at a time; its first logits are requested before the length and the statistics are there (the call's second launch: 8 x 8191 slots,
 // 32 heads: 5 us).
 __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const float* __restrict__ logits, const float2* __restrict__ stat,
                                                             int logit_stride, float* __restrict__ weights)
@@ -740,7 +740,8 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------
 // A list's n_keep slots of the largest keys, and the moves that bring them below slot n_keep.  One workgroup per list; a wave holds
-// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps (32768 slots; longer lists, and few of more than 16384 slots, further below).
+// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps (32768 slots; longer lists, and few of more than 16384
+// slots, further below).
 //
 // Threshold: the key and the slot of the last one that stays.  Where up to kEvFew leave they are found one by one (the lowest first).
 // Otherwise a histogram over the keys' leading 12 bits (keys are the floats' bits in order, so eight bins for a factor of two) names the

@@ -19,7 +19,6 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline bool bad(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline sals_status launch_status() { return hipGetLastError() == hipSuccess ? SALS_OK : SALS_ERR_HIP; }
 
-
 struct PagedLayout {  // byte offsets into the workspace
     size_t count, sum, stat, final_stat, logits, moves, from, to, hist, n_cand, arrived, state, cand, part, total;
     size_t n_zero;   // words from `count` on that are zero between launches
@@ -160,7 +159,8 @@ sals_status launch_attend(const sals_paged* c, const void* q, const int32_t* q_p
     const float scale = (float)(1.4426950408889634074 / std::sqrt((double)D));
     // (64 KB of LDS for runs of logits: not where no wave can have more than two blocks, 0.5 us)
     const int keep = logits && (int64_t)d.B * ceil_div(a.cap, PgBlock<T>::TB) >= 16 * (kPgGroups / (d.H_kv * L.tiles)) ? 1 : 0;
-    hipLaunchKernelGGL((attend_kernel<T, D>(c)), dim3(L.groups), dim3(kPgWaves * 64), keep ? std::max(L.lds, kPgWaves * kPgKept * 4) : L.lds, st, seq_len, d.B, a.cap, d.H_kv, L.tiles, a,
+    const int lds = keep ? std::max(L.lds, kPgWaves * kPgKept * 4) : L.lds;
+    hipLaunchKernelGGL((attend_kernel<T, D>(c)), dim3(L.groups), dim3(kPgWaves * 64), lds, st, seq_len, d.B, a.cap, d.H_kv, L.tiles, a,
                        static_cast<const T*>(q), q_pos, static_cast<const T*>(Kp), static_cast<const T*>(Vp), static_cast<T*>(out), parts, logits,
                        L.logit_stride, keep, scale, c->log2_theta, d.rope_style);
     if (launch_status() != SALS_OK || !weights) return launch_status();

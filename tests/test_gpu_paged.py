@@ -625,3 +625,16 @@ def test_binding_refuses_what_does_not_fit():
     c.ctx.close()
     with pytest.raises(binding.SalsError):
         c.attend()
+
+
+def test_binding_refuses_counts_of_more_than_32_bits():
+    c = Cache([20, 30], lists=2)
+    state = lambda: [t.clone().contiguous().view(torch.uint8) for t in (c.seq_len, c.pos, c.weights, c.Kp)]   # (as bits: the pools hold NaN)
+    before = state()
+    for counts in ((2 ** 32 + 5, 0, 0), (8, 2 ** 32, 0), (8, 0, 2 ** 31), (-1, 0, 0), (8, -2 ** 32, 0)):
+        with pytest.raises(binding.SalsError):
+            c.ctx.evict(c.q_pos, c.table, c.Kp, c.Vp, c.seq_len, c.pos, c.weights, *counts)
+    for n_tok in (0, -1, 2 ** 32 + 1):
+        with pytest.raises(binding.SalsError):
+            c.ctx.append(c.q[:, :2], c.q[:, :2], c.q_pos, c.table, c.Kp, c.Vp, c.seq_len, n_tok=n_tok, pos=c.pos, weights=c.weights)
+    assert all(torch.equal(x, y) for x, y in zip(before, state()))
