@@ -258,8 +258,9 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     W.blocks = __builtin_amdgcn_readlane((int)upto, 63);
     // Two neighbouring KV heads of a workgroup, four waves for each, read longer pieces of memory, and the channels that are slow for every
     // fourth 256 bytes are shared out; a sequence then has twice as many pieces to join.  Worth it from 16 blocks for each workgroup on,
-    // where a sequence has no more than about 16 pieces or is long (32 heads, 16 x 4096 slots: 177 -> 167 us; 8 heads, 8 x 8191: 62 -> 60;
-    // 1 x 4100: 13.7, with two 18.7; 1 x 32768: 30, with two 34).  Four with two waves each: 172, and no faster for heads of 64 channels.
+    // where a sequence has no more than about 16 pieces or is long (32 heads, 16 x 4096 slots: 177 -> 165 us; 8 heads, 8 x 8191: 51.7 ->
+    // 50.0; 32 of 188 to 6002: 76.7 -> 71.8; 1 x 4100: 12.8, with two 18.0; 1 x 32768: 28.2, with two 32.2).  Four with two waves each: 172,
+    // and no faster for heads of 64 channels.
     const int single = kv_heads * tiles, per_group = idiv(kPgGroups, single);
     const int lg = tiles == 1 && !(kv_heads & 1) && W.blocks >= 16 * per_group && (2 * per_group <= 16 * B || W.blocks >= 128 * per_group) ? 1 : 0;
     const int HPW = 1 << lg, WPH = kPgWaves >> lg, heads = single >> lg;
@@ -276,8 +277,9 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
     }
     if (w >= W.shares) return;
     // A sequence that begins in a share costs it the end of one stream and the start of another, as much as some blocks, which are dealt
-    // with the real ones (32 sequences of 188 to 6002 slots: 78.6 -> 74.4 us, with 4 to 16 of them alike); not where all are equally long and
-    // whole numbers of shares (8 x 8191 slots: 67.5, with them 68.4).
+    // with the real ones: up to 4 (up to 1, 2, 4, 8 and 16 of them: 32 sequences of 188 to 6002 slots 74.6, 73.2, 72.4, 75.6 and 77.7 us, 256
+    // of up to 800 slots 87.6, 86.4, 86.6, 88.6 and 92.7); not where all are equally long and whole numbers of shares (8 x 8191 slots:
+    // 50.0, with them 51.2).
     int pad = 0;
     W.q = W.per_share(W.blocks, W.shares);
     if (W.q >= 8) {
