@@ -134,8 +134,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
 //   O^T += V^T p^T   rows = channels, contraction over slots: the lane that holds the weights of slots c CH .. c CH + CH - 1 of head n
 //                    (the layout that S^T leaves, with the slots of K's rows dealt accordingly) needs the same slots of channel n of V;
 //                    it loads 16 (8) bytes of each of their rows and byte permutes turn them, so nothing passes through LDS.
-// bf16: the rotated query is three bf16 pieces (exact to fp32's own rounding), a weight a head cut off and a remainder (2^-14 of it
-// lost at most), products and sums fp32.  The remainder is never zero beside a nonzero head: an infinite value stays one.
+// bf16: the rotated query is three bf16 pieces (exact to fp32's own rounding), and so is a weight (split3); products and sums fp32.
+// None of a weight's pieces is zero unless the weight is: an infinite value stays one.  (With two pieces, 16 bits of a weight, outputs were off
+// by 3e-6 before their rounding, ten times what the sums take.)
 // A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
 constexpr int kPgWaves = 8;
@@ -192,6 +193,21 @@ __device__ __forceinline__ void st2_device(float2* p, float2 v)
 {
     __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// x >= 0 as three floats of 8 significant bits: its sum exactly, every piece above zero where x is (from 2^-103 on).  Pieces are cut off from
+// what is one step below, so that something is left of a power of two, or of any number that has the piece's bits alone.  The upper
+// halves are the pieces in bf16 (the lower halves of the first two are to be dropped).
+struct Split3 { uint32_t x0, x1, x2; };
+__device__ __forceinline__ Split3 split3(float x)
+{
+    Split3 s;
+    s.x0 = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u);
+    const float r = x - __uint_as_float(s.x0 & 0xffff0000u);
+    s.x1 = __builtin_elementwise_sub_sat(__float_as_uint(r), 1u);
+    s.x2 = __float_as_uint(r - __uint_as_float(s.x1 & 0xffff0000u));
+    return s;
+}
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
+
 __device__ __forceinline__ void device_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // a barrier for what was written to LDS; loads on their way stay there
@@ -517,22 +533,22 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                 }
             }
             if constexpr (BF) {
-                u32x4 ph, pl;
+                u32x4 pw[3];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const uint32_t u0 = __float_as_uint(p[2 * k]), u1 = __float_as_uint(p[2 * k + 1]);
-                    ph[k] = __builtin_amdgcn_perm(u1, u0, 0x07060302);
-                    const float r0 = fmaxf(p[2 * k] - __uint_as_float(u0 & 0xffff0000u), p[2 * k] * 0x1p-20f);
-                    const float r1 = fmaxf(p[2 * k + 1] - __uint_as_float(u1 & 0xffff0000u), p[2 * k + 1] * 0x1p-20f);
-                    pl[k] = (uint32_t)f32_to_bf16(r0) | (uint32_t)f32_to_bf16(r1) << 16;
+                    const Split3 a0 = split3(p[2 * k]), a1 = split3(p[2 * k + 1]);
+                    pw[0][k] = upper_halves(a0.x0, a1.x0);
+                    pw[1][k] = upper_halves(a0.x1, a1.x1);
+                    pw[2][k] = upper_halves(a0.x2, a1.x2);
                 }
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     u32x4 v;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_perm(V[2 * k + 1][j >> 1], V[2 * k][j >> 1], j & 1 ? 0x07060302 : 0x05040100);
-                    O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pl), O[j], 0, 0, 0);
-                    O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, ph), O[j], 0, 0, 0);
+#pragma unroll
+                    for (int k = 2; k >= 0; --k)
+                        O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pw[k]), O[j], 0, 0, 0);
                 }
             } else {
 #pragma unroll

@@ -1,0 +1,64 @@
+"""GPU tests of what the paged cache's attention makes of single values: weights in full fp32, infinite and undefined keys and values.
+
+eps = 2^-24 is half a step of fp32."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from oracle import paged_oracle as po  # noqa: E402
+from test_gpu_paged import DEV, EPS, HALF, Cache, _np  # noqa: E402
+
+
+def _small(keys, values, d, dtype, H=1, H_kv=1, P=16):
+    """Slots whose keys are `keys` in channel 0 and zero elsewhere, values `values` in all channels; a query of ones in channel 0 at position
+    0: logit j is keys[j] / sqrt(d)."""
+    n = len(keys)
+    c = Cache([n], H=H, H_kv=H_kv, d=d, P=P, dtype=dtype)
+    K = torch.zeros(n, H_kv, d)
+    K[:, :, 0] = torch.tensor(keys)[:, None]
+    V = torch.as_tensor(values, dtype=torch.float32)[:, None, None].expand(n, H_kv, d)
+    page, row, _ = po.slots(c.table_h[0], P, n, c.n_pages)
+    at = torch.from_numpy(page).long().to(DEV), torch.from_numpy(row).long().to(DEV)
+    c.Kp[at] = K.to(c.Kp.dtype).to(DEV)
+    c.Vp[at] = V.to(c.Vp.dtype).to(DEV)
+    c.q.zero_()
+    c.q[:, :, 0] = 1.0
+    c.q_pos.zero_()
+    return c
+
+
+# exp(k / 8) of these needs more than 16 bits: a head of 8 and a rounded remainder of 8 are off by 0.57 to 0.95 2^-16 of it, too much ...
+TOO_MUCH = [-1.6796875, -4.03125, -3.109375, -2.03125, -3.375, -3.734375, -2.875, -5.25, -3.875, -5.5, -5.375]
+# ... and too little
+TOO_LITTLE = [-3.78125, -4.40625, -4.90625, -4.28125, -3.421875, -2.96875, -2.6875, -4.625, -3.09375, -2.359375, -3.25]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("copies", [1, 20])
+def test_weights_enter_the_sum_in_full(dtype, copies):
+    """Values +1 where 16 bits of a weight are too much and -1 where they are too little, and two values that cancel the sum to 2^-17 of
+    it, so that the output's own rounding hides nothing.
+
+    Bound, relative to sum p |v|: a logit takes a rounding of the scale, one of the scaled query and two of its three products with the key, of
+    at most 5.5 / 8 log2(e) = 1: 4 eps ln 2 of the weight; exp2 2 eps; the sum, of three products a slot, one rounding each, 3 n eps at
+    most for the n slots of a wave (and n = 23 in a block of 32) and 10 for joining the waves."""
+    keys = (TOO_MUCH + TOO_LITTLE) * copies + [0.0, 0.0]
+    sign = np.array(([1.0] * len(TOO_MUCH) + [-1.0] * len(TOO_LITTLE)) * copies)
+    p = np.exp(np.array(keys) / 8.0)
+    first = -float(torch.tensor(np.sum(p[:-2] * sign)).to(torch.bfloat16))
+    second = -float(torch.tensor(np.sum(p[:-2] * sign) + first).to(torch.bfloat16))
+    v = np.concatenate([sign, [first, second]])
+    c = _small(keys, v, 64, dtype)
+    c.attend()
+    torch.cuda.synchronize()
+    want, size = np.sum(p * v) / p.sum(), np.sum(p * np.abs(v)) / p.sum()
+    assert abs(want) < 2.0 ** -16 * size     # (the premise)
+    bound = (4 * np.log(2) + 2 + 3 * min(len(keys), 32) + -(-len(keys) // 16) + 10) * EPS * size + HALF[dtype] * abs(want)
+    err = np.abs(_np(c.out)[0, 0] - want)
+    print(f"    error {err.max() / size * 2 ** 16:.4f} 2^-16 of the sum, bound {bound / size * 2 ** 16:.4f}", flush=True)
+    assert (err <= bound).all()
