@@ -627,8 +627,8 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
             for (int v = 1; v < kPgWaves; ++v) Mh = fmaxf(Mh, mv[v]);
 #pragma unroll
             for (int v = 0; v < kPgWaves; ++v)
-                if (v < n_live && lv[v] != 0.f) {   // (or a NaN, which is to stay)
-                    const float f = __builtin_amdgcn_exp2f(mv[v] - Mh);
+                if (v < n_live) {   // (a sum of weight zero counts too: what is not finite in it is to stay)
+                    const float f = lv[v] != 0.f ? __builtin_amdgcn_exp2f(mv[v] - Mh) : 0.f;
                     L = fmaf(lv[v], f, L);
                     A += ov[v] * f;
                 }
@@ -695,7 +695,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
 #pragma unroll
                             for (int u = 0; u < kPgAhead; ++u)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) A[e] = fmaf(f[u] != 0.f ? x[u][e] : 0.f, f[u], A[e]);   // (x is zero behind the last piece)
+                                for (int e = 0; e < 4; ++e) A[e] = fmaf(x[u][e], f[u], A[e]);   // (x is zero behind the last piece)
                         }
                         if (sharers == 1) finish(quad, A, sM[hh / kPgHeads][hh % kPgHeads], sL[hh / kPgHeads][hh % kPgHeads]);
                     }

@@ -62,3 +62,21 @@ def test_weights_enter_the_sum_in_full(dtype, copies):
     err = np.abs(_np(c.out)[0, 0] - want)
     print(f"    error {err.max() / size * 2 ** 16:.4f} 2^-16 of the sum, bound {bound / size * 2 ** 16:.4f}", flush=True)
     assert (err <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [44, 300, 4096, 30000])
+def test_values_of_weight_zero_that_are_not_finite_show(dtype, n):
+    """A value row far below the largest logit has weight zero in fp32; zero times NaN or infinity is a NaN, however the sequence is spread
+    over waves and workgroups."""
+    keys, values = [-2400.0] * 40 + [0.0] * (n - 40), [1.0] * n      # (logits -300 and 0)
+    c = _small(keys, values, 64, dtype)
+    page, row, _ = po.slots(c.table_h[0], c.P, n, c.n_pages)
+    c.Vp[int(page[5]), int(row[5]), 0, 3] = float("nan")
+    c.Vp[int(page[39]), int(row[39]), 0, 7] = float("inf")
+    c.attend()
+    torch.cuda.synchronize()
+    out = _np(c.out)[0, 0]
+    assert np.isnan(out[[3, 7]]).all()
+    # (a mean of ones: the rounding of n terms and that of the result)
+    assert (np.abs(np.delete(out, [3, 7]) - 1.0) <= HALF[dtype] + (64 + n / 32) * EPS).all()
