@@ -496,7 +496,8 @@ sals_status sals_paged_append(sals_paged* ctx, const void* k_new, const void* v_
 
 /* Dense attention of one new token per sequence over its cached slots (sals_dense_attend over pages):
  *   p[h, j]   = softmax_j( RoPE(q[b,h], q_pos[b]) . K[j, g(h)] / sqrt(d) ),  j < seq_len[b], page there
- *   out[b, h] = sum_j p[h, j] V[j, g(h)]           fp32 accumulation, one rounding to T; zero where no slot has a page
+ *   out[b, h] = sum_j p[h, j] V[j, g(h)]           fp32 accumulation, one rounding to T; zero where no slot has a page,
+ *                                                  or none a logit above -infinity
  *                                                  (weights that vanish in fp32 count: a NaN or infinity they meet gives NaN)
  *   weights[b, a, j] += sum over the query heads h of a of p[h, j]    (in head order, fp32)
  * `weights` may be NULL: then none are added up.  Results do not depend on the order in which workgroups run.

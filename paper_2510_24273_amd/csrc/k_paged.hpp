@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache a, const T
 //                    (the layout that S^T leaves, with the slots of K's rows dealt accordingly) needs the same slots of channel n of V;
 //                    it loads 16 (8) bytes of each of their rows and byte permutes turn them, so nothing passes through LDS.
 // bf16: the rotated query is three bf16 pieces (exact to fp32's own rounding), and so is a weight (split3); products and sums fp32.
-// None of a weight's pieces is zero unless the weight is: an infinite value stays one.  (With two pieces, 16 bits of a weight, outputs were off
+// No piece is zero unless the number is, and all have its sign: infinite keys and values stay what they are.  (With two pieces, 16 bits of a weight, outputs were off
 // by 3e-6 before their rounding, ten times what the sums take.)
 // A maximum is followed only when a logit exceeds it by more than 8 (in units of ln 2; weights then stay below 2^8), which few blocks need.
 constexpr int kPgHeads = 16;           // query heads of a workgroup
@@ -427,16 +427,20 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void paged_attend_kernel(const in
                 if (col >= HPW * kPgHeads) break;
                 const bool live = col % kPgHeads < nh;
                 const float x = live ? __uint_as_float(q1[k] << (BF ? 16 : 0)) : 0.f, y = live ? __uint_as_float(q2[k] << (BF ? 16 : 0)) : 0.f;
-                float r[2] = {fmaf(x, cs.x, -(y * cs.y)) * scale, fmaf(y, cs.x, x * cs.y) * scale};
+                const float r[2] = {fmaf(x, cs.x, -(y * cs.y)) * scale, fmaf(y, cs.x, x * cs.y) * scale};
                 const int ch[2] = {ch1, ch2};
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int k3 = 0; k3 < (BF ? 3 : 1); ++k3) {
-                        T* to = reinterpret_cast<T*>(&sQ[col / kPgHeads][k3][ch[u] / (4 * VEC)][ch[u] / VEC % 4 * 16 + col % kPgHeads]) + ch[u] % VEC;
-                        elem<T>::store(to, r[u]);
-                        if constexpr (BF) r[u] -= (float)(__bf16)r[u];
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t piece[3] = {__float_as_uint(r[u]), 0u, 0u};
+                    if constexpr (BF) {   // (pieces of the element's sign, none of them zero: an infinite key stays one)
+                        const Split3 s = split3(fabsf(r[u]));
+                        const uint32_t sign = __float_as_uint(r[u]) & 0x80000000u;
+                        piece[0] = (s.x0 | sign) >> 16; piece[1] = (s.x1 | sign) >> 16; piece[2] = (s.x2 | sign) >> 16;
                     }
+#pragma unroll
+                    for (int k3 = 0; k3 < (BF ? 3 : 1); ++k3)
+                        reinterpret_cast<Raw*>(&sQ[col / kPgHeads][k3][ch[u] / (4 * VEC)][ch[u] / VEC % 4 * 16 + col % kPgHeads])[ch[u] % VEC] = (Raw)piece[k3];
+                }
             }
         }
         lds_barrier();

@@ -80,3 +80,41 @@ def test_values_of_weight_zero_that_are_not_finite_show(dtype, n):
     assert np.isnan(out[[3, 7]]).all()
     # (a mean of ones: the rounding of n terms and that of the result)
     assert (np.abs(np.delete(out, [3, 7]) - 1.0) <= HALF[dtype] + (64 + n / 32) * EPS).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [3, 700])
+def test_an_infinite_key_is_a_logit_like_others(dtype, d, n):
+    """A key with an infinity against a query of the other sign in that channel: logit -infinity, weight zero; of the same sign: NaN."""
+    c = Cache([n, 90], H=6, H_kv=2, d=d, dtype=dtype, lists=2)
+    c.q_pos.zero_()
+    c.q[0, :, 9] = torch.tensor([0.71875, 1.0, -0.34375, 0.001, 2.0, 3.0], dtype=c.q.dtype, device=DEV)
+    page, row, _ = po.slots(c.table_h[0], c.P, n, c.n_pages)
+    at = int(page[1]), int(row[1])
+    c.Kp[at[0], at[1], :, 9] = -float("inf")
+    before = c.weights.clone()
+    c.attend()
+    torch.cuda.synchronize()
+    out, added = _np(c.out), _np(c.weights - before)[0]
+    assert np.isnan(out[0, 2]).all()                       # (its logit is +infinity)
+    assert np.isfinite(np.delete(out[0], 2, axis=0)).all() and np.isfinite(out[1]).all()
+    assert added[1, 1] == 0.0 and np.isfinite(added[1]).all() and np.isnan(added[0, :n]).all()
+    # the others' rows as if that slot were not there
+    K, there = c.rows(c.Kp, 0, n)
+    V, _ = c.rows(c.Vp, 0, n)
+    K[1], there[1] = 0.0, False
+    want, p = po.attend(_np(c.q[0]), 0, K, V, there, c.theta)
+    size = np.einsum("hn,nhc->hc", p, np.repeat(np.abs(V), 3, axis=1))
+    logit = np.einsum("hc,nhc->hn", np.abs(_np(c.q[0])), np.repeat(np.abs(K), 3, axis=1)).max(axis=1) / np.sqrt(d)
+    # (a logit: d + 16 roundings of at most the sum of its products; weights twice that; the sum of n terms; the output's rounding)
+    bound = HALF[dtype] * np.abs(want) * (1 + 2.0 ** -6) + ((2 * (d + 16) * logit + 2 * (64 + n / 32)) * EPS + 2.0 ** -19)[:, None] * size
+    for h in (0, 1, 3, 4, 5):
+        assert (np.abs(out[0, h] - want[h]) <= bound[h]).all(), h
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_sequence_whose_logits_are_all_minus_infinity_is_zero(dtype):
+    c = _small([-float("inf")] * 40, [1.0] * 40, 64, dtype)
+    c.attend()
+    torch.cuda.synchronize()
+    assert not _np(c.out).any()
