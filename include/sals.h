@@ -442,7 +442,7 @@ sals_status sals_calib_eigenvectors(double* C, int32_t D, int32_t r, int32_t dty
  *   table [B, max_pages] int32:  table[b, j / page_size].
  * seq_len[b] slots are in use (seq_len is clamped to [0, max_pages * page_size]).  An entry outside [0, n_pages) is a
  * page that is not there: append drops the tokens that belong there (their slots are counted), attend gives them no weight,
- * evict neither reads nor writes their rows.  Entries of slots at or past the length are not read by attend.
+ * evict neither reads nor writes their rows (and is not for sequences that have such slots, see there).  Entries of slots at or past the length are not read by attend.
  * The context holds no cache state: one context serves all layers of a shape.
  *
  * Accumulated attention weights (weight_heads: 0 none, 1 one per slot, H_kv one per slot and KV head):
@@ -513,6 +513,9 @@ sals_status sals_paged_attend(sals_paged* ctx, const void* q, const int32_t* q_p
  * i-th of the ones into the i-th of the others in slot order: rows of K and V, pos and weights.  Then
  * seq_len[b] = n_keep, and the pages from slot n_keep on may be given to other sequences.  Nothing else is written; a
  * sequence of at most n_keep slots stays as it is.  Pages that more than one sequence reads must not be among those moved into.
+ * Every slot below the length should have a page.  The ranking does not look at pages, and a move from or to a slot without one takes
+ * pos, weights and src along but no rows: a token that moves into a slot without a page is lost to attend, and where a slot without
+ * a page moves into one that has a page, the row of the token that was evicted stays and is attended to under the moved one's entry.
  *   q_pos  [B] int32                          position of the sequence's newest token
  *   n_keep 1 .. max_pages * page_size;  n_sink, n_recent >= 0 (host)
  *   src    [B, weight_heads, n_keep] int32    out, may be NULL: the slot that the token now in slot j came from; -1 from

@@ -118,3 +118,42 @@ def test_a_sequence_whose_logits_are_all_minus_infinity_is_zero(dtype):
     c.attend()
     torch.cuda.synchronize()
     assert not _np(c.out).any()
+
+
+@pytest.mark.parametrize("lists", [1, 3])
+def test_an_eviction_of_a_sequence_with_missing_pages_and_attention_behind_it(lists):
+    """What the header says of it: entries move by rank alone; rows only between slots with pages.  Attention behind it gives the slots
+    without pages no weight and takes the others' rows as they lie there."""
+    c = Cache([120], H=6, H_kv=3, d=64, P=10, lists=lists, holes=[(0, 1, -1), (0, 8, -1)])   # slots 10 .. 19 and 80 .. 89
+    keep = 50
+    c.q_pos.fill_(119)
+    c.pos.copy_(torch.arange(120, dtype=torch.int32, device=DEV).expand(1, lists, 120))
+    w = torch.rand(1, lists, 120, generator=torch.Generator().manual_seed(9)) + 0.5
+    w[..., 0:30] = 0.001         # free slots, 10 .. 19 without pages; kept ones behind move into them, 80 .. 89 among these
+    w[..., 60:90] = 5.0
+    c.weights.copy_(w)
+    K0, V0, page, row, there = c.Kp.clone(), c.Vp.clone(), *po.slots(c.table_h[0], 10, 120, c.n_pages)
+    src = torch.empty((1, lists, keep), dtype=torch.int32, device=DEV)
+    c.ctx.evict(c.q_pos, c.table, c.Kp, c.Vp, c.seq_len, c.pos, c.weights, keep, src=src)
+    torch.cuda.synchronize()
+    assert c.seq_len.tolist() == [keep]
+    lost = stale = 0
+    for a in range(lists):
+        line = po.evict(w[0, a].numpy(), np.arange(120), 119, keep, 0, 0)
+        assert src[0, a].tolist() == line == c.pos[0, a, :keep].tolist()
+        assert torch.equal(c.weights[0, a, :keep].cpu(), w[0, a, line])
+        heads = slice(None) if lists == 1 else slice(a, a + 1)
+        for j, x in enumerate(line):
+            if there[j]:
+                frm = x if there[x] else j
+                for new, old in ((c.Kp, K0), (c.Vp, V0)):
+                    assert torch.equal(new[int(page[j]), int(row[j]), heads], old[int(page[frm]), int(row[frm]), heads])
+            lost += bool(not there[j] and there[x])
+            stale += bool(there[j] and not there[x])
+    assert lost and stale        # (the premise)
+    c.lens = [keep]
+    before = c.weights.clone()
+    c.attend()
+    torch.cuda.synchronize()
+    c.check_attend(before)
+    assert torch.equal(c.weights[..., 10:20], before[..., 10:20])
