@@ -1,4 +1,4 @@
-"""GPU tests of the eviction where there are many lists."""
+"""GPU tests of the eviction where there are many lists, and of all three calls on pools past 2^32 elements."""
 import numpy as np
 import pytest
 
@@ -10,7 +10,7 @@ if not torch.cuda.is_available():
 
 from oracle import paged_oracle as po  # noqa: E402
 from paper_2510_24273_amd import binding  # noqa: E402
-from test_gpu_paged import DEV  # noqa: E402
+from test_gpu_paged import DEV, Cache, _positions  # noqa: E402
 
 
 def _line(w, pos, position, keep, sink, recent):
@@ -72,3 +72,47 @@ def test_many_long_lists(B, H_kv, lists, cap, P, gone, kind):
     if B == 8:   # (the sort against the oracle)
         n = lens[1]
         assert want[1, 3].tolist() == po.evict(w_h[1, 3, :n], p_h[1, 3, :n], 2 * cap - 1, keep, 16, 100)
+
+
+@pytest.mark.parametrize("lists", [1, 8])
+def test_offsets_past_32_bits_of_elements(lists):
+    """Pages 2 MiB apart in a pool of 4.4e9 elements, of which the cache has the last: append, attend and evict leave what they leave in a
+    small pool."""
+    P, H_kv, d, n_pages, stride = 16, 8, 128, 4300, 1 << 20
+    pool = torch.empty(n_pages * stride, dtype=torch.bfloat16, device=DEV)
+    Kp = pool.as_strided((n_pages, P, H_kv, d), (stride, H_kv * d, d, 1))
+    Vp = pool[P * H_kv * d:].as_strided((n_pages, P, H_kv, d), (stride, H_kv * d, d, 1))
+    small = Cache([200, 97], H=16, H_kv=H_kv, P=P, lists=lists, mp=14)
+    _positions(small)
+    first = n_pages - 2 * small.mp
+    assert first * stride > 2 ** 32
+    table = torch.arange(2 * small.mp, dtype=torch.int32, device=DEV).view(2, small.mp) + first
+    used, at = small.table.view(-1).long(), table.view(-1).long()
+    Kp[at], Vp[at] = small.Kp[used], small.Vp[used]
+    ctx = binding.Paged(binding.make_paged_desc(2, 16, H_kv, d, P, small.mp, n_pages, "bf16", weight_heads=lists, page_stride=stride), DEV)
+    pos, weights, seq_len, out = small.pos.clone(), small.weights.clone(), small.seq_len.clone(), torch.empty_like(small.out)
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(2, 5, H_kv, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    bits = lambda t: t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+    def same():
+        torch.cuda.synchronize()
+        for x, y in ((Kp[at], small.Kp[used]), (Vp[at], small.Vp[used]), (pos, small.pos), (weights, small.weights), (seq_len, small.seq_len)):
+            assert torch.equal(bits(x), bits(y))
+
+    q_pos = small.q_pos
+    same()
+    ctx.append(k, v, q_pos, table, Kp, Vp, seq_len, n_tok=5, pos=pos, weights=weights)
+    small.ctx.append(k, v, q_pos, small.table, small.Kp, small.Vp, small.seq_len, n_tok=5, pos=small.pos, weights=small.weights)
+    same()
+    assert seq_len.tolist() == [205, 102]
+    small.lens = [205, 102]
+    ctx.attend(small.q, q_pos, table, Kp, Vp, seq_len, out, weights=weights)
+    small.attend()
+    same()
+    small.check_attend()
+    assert torch.equal(bits(out), bits(small.out))
+    ctx.evict(q_pos, table, Kp, Vp, seq_len, pos, weights, 90, n_sink=4, n_recent=10)
+    small.ctx.evict(q_pos, small.table, small.Kp, small.Vp, small.seq_len, small.pos, small.weights, 90, n_sink=4, n_recent=10)
+    same()
+    assert seq_len.tolist() == [90, 90]
