@@ -7,15 +7,17 @@ namespace sals {
 
 // 16 bytes per lane from `src` straight into LDS at `lds_base` + 16 * lane (lds_base: byte offset of the wave's piece, wave
 // uniform).  Inline assembly, so that the compiler does not order later LDS reads behind it: the caller counts the
-// outstanding loads (vm_wait) and separates writers from readers with a barrier.
+// outstanding loads (vm_wait) and separates writers from readers with a barrier.  The instruction between the write of m0 and the load
+// that goes by it is one that the hardware asks for (it does not wait there by itself; the compiler puts one in its own code): a load right
+// behind may go by the old m0, to the place of the one before.
 __device__ __forceinline__ void load_lds16(const void* src, uint32_t lds_base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src) : "memory");
 }
 // the same from a wave-uniform base and a 32-bit offset per lane
 __device__ __forceinline__ void load_lds16(const void* base, uint32_t offset, uint32_t lds_base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(offset), "s"(base) : "memory");
 }
 template <int N> __device__ __forceinline__ void vm_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wg_barrier()
