@@ -2169,7 +2169,7 @@ sals_status sals_calib_eigenvectors(double* C, int32_t D, int32_t r, int32_t dty
         hipLaunchKernelGGL(calib_chol_finish_kernel, dim3(D), dim3(256), 0, st, G, D, diag);
         return launch_status() == SALS_OK;
     };
-    EigHost host;   // (behind the first launch a lack of memory would leave kernels at work in the caller's)
+    EigHost host(st != nullptr);   // (behind the first launch a lack of memory would leave kernels at work in the caller's; a stream is the runtime's)
     if (!host.p) return SALS_ERR_HIP;
     // G = Cholesky factor of C + shift I, the shift from C's scale, which the host learns with what came of it.
     row_norms(C);
