@@ -43,7 +43,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    flags = HIPCC_FLAGS + os.environ.get("SALS_EXTRA_FLAGS", "").split()
+    added = os.environ.get("SALS_EXTRA_FLAGS", "").split()   # (for the link as well: sanitizers, libraries)
+    flags = HIPCC_FLAGS + added
     with tempfile.TemporaryDirectory() as tmp:   # the sources side by side, then one link in the order of their names
         jobs, objs = [], []
         for src in sources():
@@ -55,7 +56,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
         failed = [(cmd, p.returncode) for cmd, p in jobs if p.wait() != 0]
         if failed:
             raise subprocess.CalledProcessError(failed[0][1], failed[0][0])
-        subprocess.run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs, check=True)
+        subprocess.run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs + added, check=True)
     return LIB
 
 
