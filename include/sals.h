@@ -420,6 +420,8 @@ sals_status sals_overlap_score(sals_ctx* ctx, const void* q, const int32_t* q_po
  *   sweeps     host int32, out (may be NULL): sweeps run; the negative of that number if the limit was reached
  *              before convergence (the results are then the current approximation); 0 if there was nothing to
  *              rotate (C is zero, or not finite: then its rows come back as they are)
+ * Sums are made in an order of their own, whatever runs beside them, and equal calls are tested to give equal bits; what is promised is
+ * that they agree as any two converged results do, to about 1e-11 of an eigenvalue.
  * BLOCKING: it waits for hip_stream at least once per sweep to read the convergence measure (and after each factorisation: one,
  * or a few for a C that rounding has left indefinite), so it cannot be captured.
  * Errors as above. */
