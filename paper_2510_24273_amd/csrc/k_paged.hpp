@@ -751,7 +751,8 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
                 if (h + u < nh) {
                     const float2 st = sStat[h + u];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(__builtin_amdgcn_exp2f(x[u][e] - st.x), st.y, sum[e]);
+                    for (int e = 0; e < 4; ++e)   // (slots without a page get nothing, be the others' weights NaN)
+                        sum[e] = x[u][e] != -INFINITY ? fmaf(__builtin_amdgcn_exp2f(x[u][e] - st.x), st.y, sum[e]) : sum[e];
                 }
         }
 #pragma unroll

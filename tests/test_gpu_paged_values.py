@@ -157,3 +157,17 @@ def test_an_eviction_of_a_sequence_with_missing_pages_and_attention_behind_it(li
     torch.cuda.synchronize()
     c.check_attend(before)
     assert torch.equal(c.weights[..., 10:20], before[..., 10:20])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lists", [1, 2])
+def test_slots_without_a_page_get_no_weight_beside_a_nan(dtype, lists):
+    c = Cache([200, 90], dtype=dtype, lists=lists, holes=[(0, 1, -1), (0, 12, 2 ** 31 - 1)])   # slots 16 .. 31 and 192 .. 199
+    c.Kp[int(c.table_h[0, 0]), 3, 1, 5] = float("nan")
+    before = c.weights.clone()
+    c.attend()
+    torch.cuda.synchronize()
+    w, was = _np(c.weights), _np(before)
+    for gone in (slice(16, 32), slice(192, None)):
+        assert np.array_equal(w[0, :, gone], was[0, :, gone])
+    assert np.isnan(w[0, -1, :16]).all() and np.isnan(w[0, -1, 32:192]).all() and np.isfinite(w[1]).all()
