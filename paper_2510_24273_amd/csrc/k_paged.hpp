@@ -763,8 +763,8 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(PagedCache a, const 
 
 // ---- eviction -------------------------------------------------------------------------------------------------------------------
 // A list's n_keep slots of the largest keys, and the moves that bring them below slot n_keep.  One workgroup per list; a wave holds
-// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps (32768 slots; longer lists, and few of more than 16384
-// slots, further below).
+// consecutive slots, 256 at a step (four for each lane), in registers up to 8 steps (tables of 32768 slots; longer ones, and those of more than
+// 16384 with few lists, further below).
 //
 // Threshold: the key and the slot of the last one that stays.  Where up to kEvFew leave they are found one by one (the lowest first).
 // Otherwise a histogram over the keys' leading 12 bits (keys are the floats' bits in order, so eight bins for a factor of two) names the
@@ -1166,13 +1166,13 @@ __global__ __launch_bounds__(kEvThreads) void paged_evict_select_kernel(PagedCac
     evict_select<T, NC>(sh, a, e, Kp, Vp, seq_len, blockIdx.x);
 }
 
-// ---- longer lists: a workgroup for each 4096 slots, in three launches (a list's keys are too many instructions for one compute unit:
+// ---- longer tables: a workgroup for each 4096 slots, in three launches (a list's keys are too many instructions for one compute unit:
 // 4 x (82 000 of 4 lists) 47 us in one workgroup each) ----
 // hist     the chunks' histograms of the leading 12 bits added up for the list; the last chunk to arrive finds the bin
-// (split   lists of more than 131072 slots: the same with the next 12 bits, if the bin has more members than a workgroup ranks)
+// (split   tables of more than 131072 slots: the same with the next 12 bits, if the bin has more members than a workgroup ranks)
 // members  every chunk counts what is certain to become free or to move, and lists the bin's members; the last one ranks them and
 //          leaves the threshold and the chunks' places in the lists of moves.  A list with more members than that (one weight many times
-//          over) is done by that workgroup alone.
+//          over, or a bin that holds many: uniform weights in 65536 slots) is done by that workgroup alone.
 // emit     every chunk writes its part of the lists of moves
 constexpr int kEvCand = 4096;
 constexpr int kEvMaxChunks = (1 << 20) / kEvChunk;

@@ -68,9 +68,9 @@ PagedLayout make_layout(const sals_paged_desc& d)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += align_up(bytes); return r; };
     const size_t rows = (size_t)d.B * d.weight_heads;
-    // Eviction of long lists, a workgroup for each chunk of 4096 slots: beyond 32768 slots, and beyond 16384 as long as there are fewer lists
-    // than keep the compute units busy (32000 slots: 1 list 43 -> 28 us, 4 lists 49 -> 35, 64 lists 72 -> 74, 256 lists 191 -> 268;
-    // 16000 slots: 32 and 30, 37 and 36).
+    // Eviction in long tables, a workgroup for each chunk of 4096 slots: beyond 32768 slots, and beyond 16384 as long as there are fewer lists
+    // than keep the compute units busy (32000 slots in use: 1 list 43 -> 28 us, 4 lists 49 -> 35, 64 lists 72 -> 74, 256 lists 191 -> 268;
+    // 16000 slots: 32 and 30, 37 and 36).  By the table, as lengths are on the device: short sequences in long tables take this way too.
     L.chunks = (int)cap > 8 * kEvChunk || ((int)cap > 4 * kEvChunk && rows < 64) ? ceil_div((int)cap, kEvChunk) : 0;
     L.count = take((size_t)d.B * single * 4);
     if (rows && L.chunks) {
