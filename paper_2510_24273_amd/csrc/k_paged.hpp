@@ -193,7 +193,7 @@ __device__ __forceinline__ void st2_device(float2* p, float2 v)
 {
     __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// x >= 0 as three floats of 8 significant bits: its sum exactly, every piece above zero where x is (from 2^-103 on).  Pieces are cut off from
+// x >= 0 as three floats of 8 significant bits: its sum exactly, every piece above zero where x is (from 2^-95 on).  Pieces are cut off from
 // what is one step below, so that something is left of a power of two, or of any number that has the piece's bits alone.  The upper
 // halves are the pieces in bf16 (the lower halves of the first two are to be dropped).
 struct Split3 { uint32_t x0, x1, x2; };
